@@ -277,6 +277,140 @@ santa_status_t santa_decode_flash(const void *q, const santa_kv_t *kv, const san
                                   int32_t *idx_out, void *out, void *ws, size_t ws_bytes,
                                   void *stream);
 
+/* ---------------------------------------------------------------------------
+ * New tokens: rotary positions, cache store, attention of a chunk
+ * ---------------------------------------------------------------------------
+ * The decode calls attend over a cache that holds the current token.  The calls
+ * below bring tokens into that cache and attend with them: any number of new
+ * tokens per sequence, of a prompt or of a part of it as well as one at a time.
+ *
+ * santa_chunk_t: the new tokens of a batch.  Sequence b's are rows q_start[b] ..
+ * q_start[b + 1] - 1 of the row buffers (q, k, v, out: one row per token) and
+ * take the LAST positions of its ctx_len[b] keys (n_k without ctx_len): with c
+ * tokens, token i stands at position ctx_len[b] - c + i, so one token stands
+ * where the decode calls have the current one.  A sequence may have none.  Rows
+ * from q_start[batch] to num_tokens - 1 hold no token: they are not read and
+ * their output rows are left as they were (a batch padded to a captured
+ * graph's size).
+ *   q_start:    device int32 [batch + 1], non-decreasing, q_start[0] >= 0; or
+ *               NULL: one token per sequence, num_tokens == batch.
+ *   num_tokens: rows of the buffers, >= q_start[batch].
+ *   max_tokens: the most tokens that a sequence is expected to have (host
+ *               value; 0 = unknown).  It chooses the kernel, and no result
+ *               depends on it. */
+typedef struct {
+  const int32_t *q_start;
+  int32_t num_tokens;
+  int32_t max_tokens;
+} santa_chunk_t;
+
+/* Sliding window with sinks: the token at position p sees position j <= p if
+ * j > p - window or j < sinks.  window >= 1 (it counts the token itself),
+ * sinks >= 0.  Cache rows that no token of the call sees are not read, nor are
+ * their block-table entries, so pages wholly between sinks and window may be
+ * freed. */
+typedef struct {
+  int32_t window;
+  int32_t sinks;
+} santa_window_t;
+
+/* Rotary frequencies.  Pair i < rotary_dim / 2 turns by f_i radians per
+ * position, f_i = theta^(-2 i / rotary_dim), changed for long contexts by
+ *   SANTA_ROPE_LINEAR  f_i / factor;
+ *   SANTA_ROPE_BASE    theta replaced by theta * factor^(R / (R - 2)), R = rotary_dim;
+ *   SANTA_ROPE_BANDS   by the turns n_i = original_len * f_i / (2 pi) that the
+ *                      pair makes over the original context: f_i for n_i >= high,
+ *                      f_i / factor for n_i <= low, linear in n_i between;
+ *   SANTA_ROPE_RAMP    f_i for pairs below d(high), f_i / factor above d(low),
+ *                      linear in i between, d(n) = R ln(original_len / (2 pi n)) /
+ *                      (2 ln theta), rounded down (high) and up (low).
+ * gain multiplies the rotated features; 0 takes the usual one (RAMP with
+ * factor > 1: 0.1 ln factor + 1; else 1). */
+typedef enum {
+  SANTA_ROPE_PLAIN = 0,
+  SANTA_ROPE_LINEAR = 1,
+  SANTA_ROPE_BASE = 2,
+  SANTA_ROPE_BANDS = 3,
+  SANTA_ROPE_RAMP = 4
+} santa_rope_scaling_t;
+
+typedef struct {
+  int32_t rotary_dim;  /* a multiple of 16 in [16, 128]; later features pass through */
+  int32_t interleaved; /* 0: pair i is features (i, i + rotary_dim / 2); 1: (2 i, 2 i + 1) */
+  double theta;        /* > 1 */
+  int32_t scaling;     /* santa_rope_scaling_t */
+  double factor;       /* > 0 (PLAIN: ignored) */
+  double original_len; /* BANDS, RAMP: > 0 */
+  double low, high;    /* BANDS, RAMP: 0 < low < high */
+  double gain;
+} santa_rope_params_t;
+
+/* The plan that the call takes: made once on the host, kept by the caller. */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t interleaved;
+  float gain;
+  int32_t reserved;
+  uint64_t step[64]; /* turns per position of each pair, the fraction in units of 2^-64 */
+} santa_rope_t;
+
+/* Fill *rope from *params (host only; no stream, no device memory). */
+santa_status_t santa_rope_init(const santa_rope_params_t *params, santa_rope_t *rope);
+
+/* The new tokens' rows, in shape->dtype: element (t, h, i) of q at q + t*q_stride
+ * + h*head_dim + i, of k and v likewise (strides in elements; parts of one
+ * projection's rows are three pointers and one stride).  16-byte aligned, as
+ * every row must be.  q may be NULL (no queries).  positions (nullable, int32
+ * [num_tokens]): the positions to rotate by, where they are not the cache
+ * positions. */
+typedef struct {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t *positions;
+} santa_rows_t;
+
+/* Rotary positions and the store into the cache, in one pass: every pair (a, b)
+ * of a query or key at position p becomes gain * (a cos - b sin, b cos + a sin)
+ * at the angle p * f_i, exact in p for any p; rotated queries go to q_out
+ * ([num_tokens, num_q_heads, head_dim] contiguous; may be q itself if q is
+ * contiguous), rotated keys and the values as they are to the tokens' rows of
+ * the cache.  rope = NULL rotates nothing (q and q_out must then be NULL): a
+ * store alone.  An FP8 cache gets the E4M3 code nearest to x / scale, ties to
+ * even, saturated at +-448; NaN stays NaN.  No two tokens may name the same
+ * cache row (sequences that share pages must not store into shared ones).  A
+ * token at a position outside [0, n_k), or whose page is negative, is rotated
+ * but not stored.  kv->k_new and kv->v_new must be NULL. */
+santa_status_t santa_rope_append(const santa_rows_t *rows, const santa_kv_t *kv,
+                                 const santa_shape_t *shape, const santa_chunk_t *chunk,
+                                 const santa_rope_t *rope, void *q_out, void *stream);
+
+/* Bytes of workspace of santa_attend_chunk and (chunk = NULL: one token per
+ * sequence) santa_decode_window; window = NULL: none.  Returns 0 if the
+ * arguments are invalid.  The workspace is one of santa_workspace_init and may
+ * be shared with the other calls. */
+size_t santa_attend_workspace_size(const santa_shape_t *shape, const santa_kv_t *kv,
+                                   const santa_chunk_t *chunk, const santa_window_t *window);
+
+/* Exact attention of a chunk of new tokens over the cache, which already holds
+ * their keys and values (santa_rope_append stores them): the token at position p
+ * of sequence b sees keys 0 .. p, or with `window` (nullable) those of
+ * santa_window_t:  out = softmax(scale q K^T) V over the visible keys.
+ * q, out: [num_tokens, num_q_heads, head_dim] contiguous, 16-byte aligned,
+ * rotated as the keys are.  A row that sees no key (a token before position 0)
+ * is zero; what hidden keys and values hold, infinities and NaN too, reaches no
+ * row.  Contiguous and paged caches, every kv_dtype; kv->k_new and kv->v_new
+ * must be NULL.  santa_set_options: `splits` sets the key splits per tile, the
+ * path is ignored. */
+santa_status_t santa_attend_chunk(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,
+                                  const santa_chunk_t *chunk, const santa_window_t *window,
+                                  float scale, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* Exact decode attention with a sliding window and sinks: santa_attend_chunk
+ * with one token per sequence.  q and out as in santa_decode_dense. */
+santa_status_t santa_decode_window(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,
+                                   const santa_window_t *window, float scale, void *out, void *ws,
+                                   size_t ws_bytes, void *stream);
+
 /* Profiling hook (not part of the method).  start_event and stop_event are
  * hipEvent_t handles created by the caller with timing enabled.  The next
  * santa_decode_* (or santa_stream_read) call made on the calling thread

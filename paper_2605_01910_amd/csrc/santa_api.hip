@@ -10,6 +10,7 @@
 #include <string>
 
 #include "santa.h"
+#include "santa_chunk.h"
 #include "santa_kernels.h"
 #include "santa_plan.h"
 
@@ -85,7 +86,8 @@ santa_status_t check_shape(const santa_shape_t *sh) {
   return SANTA_OK;
 }
 
-santa_status_t check_kv(const santa_kv_t *kv, const santa_shape_t *sh, bool need_k) {
+// decode: the call is a decode step, which reads an FP8 cache on its fused paths only
+santa_status_t check_kv(const santa_kv_t *kv, const santa_shape_t *sh, bool need_k, bool decode = true) {
   if (!kv) return fail(SANTA_ERR_INVALID_ARG, "kv is NULL");
   if ((need_k && !kv->k) || !kv->v) return fail(SANTA_ERR_INVALID_ARG, "kv->k or kv->v is NULL");
   if (kv->n_k < 1) return fail(SANTA_ERR_INVALID_ARG, "n_k must be >= 1");
@@ -99,7 +101,7 @@ santa_status_t check_kv(const santa_kv_t *kv, const santa_shape_t *sh, bool need
       return fail(SANTA_ERR_INVALID_ARG, "an FP8 cache needs k_scale and v_scale");
     if (kv->k_new || kv->v_new)
       return fail(SANTA_ERR_UNSUPPORTED, "the fused append is not available with an FP8 cache");
-    if (g_opts.path == SANTA_PATH_MULTI)
+    if (decode && g_opts.path == SANTA_PATH_MULTI)
       return fail(SANTA_ERR_UNSUPPORTED, "an FP8 cache needs the fused launch layout");
   }
   const int64_t esz = fp8 ? 1 : sh->dtype == SANTA_BF16 ? 2 : 4;
@@ -249,13 +251,76 @@ santa::Plan make_plan(const santa_shape_t *sh, const santa_kv_t *kv, int S, int 
   return p;
 }
 
-santa_status_t check_ws(const santa::Plan &p, void *ws, size_t ws_bytes) {
+santa_status_t check_ws(size_t need, void *ws, size_t ws_bytes) {
   if (!ws) return fail(SANTA_ERR_WORKSPACE, "workspace is NULL");
   if (reinterpret_cast<uintptr_t>(ws) & 255) return fail(SANTA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (ws_bytes < p.total)
-    return fail(SANTA_ERR_WORKSPACE, "workspace too small: need " + std::to_string(p.total) +
+  if (ws_bytes < need)
+    return fail(SANTA_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) +
                                          " bytes, got " + std::to_string(ws_bytes));
   return SANTA_OK;
+}
+
+santa_status_t check_ws(const santa::Plan &p, void *ws, size_t ws_bytes) { return check_ws(p.total, ws, ws_bytes); }
+
+bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15; }
+
+// Chunk of new tokens (NULL: one per sequence).
+santa_status_t check_chunk(const santa_chunk_t *ch, const santa_shape_t *sh, santa_chunk_t *out) {
+  *out = ch ? *ch : santa_chunk_t{nullptr, sh->batch, 1};
+  if (out->num_tokens < 1) return fail(SANTA_ERR_INVALID_ARG, "num_tokens must be >= 1");
+  if (out->max_tokens < 0) return fail(SANTA_ERR_INVALID_ARG, "max_tokens must be >= 0");
+  if (!out->q_start) {
+    if (out->num_tokens != sh->batch)
+      return fail(SANTA_ERR_INVALID_ARG, "without q_start, num_tokens must equal batch");
+    out->max_tokens = 1;
+  }
+  return SANTA_OK;
+}
+
+santa_status_t check_window(const santa_window_t *win) {
+  if (win && (win->window < 1 || win->sinks < 0))
+    return fail(SANTA_ERR_INVALID_ARG, "window must be >= 1 and sinks >= 0");
+  return SANTA_OK;
+}
+
+santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv, const santa_chunk_t &ch,
+                                   const santa_window_t *win) {
+  santa::AttendPlan p{};
+  p.B = sh->batch;
+  p.Hq = sh->num_q_heads;
+  p.Hkv = sh->num_kv_heads;
+  p.G = p.Hq / p.Hkv;
+  p.dtype = sh->dtype;
+  p.elem = kv->kv_dtype == SANTA_KV_FP8_E4M3 ? 2 : sh->dtype == SANTA_BF16 ? 0 : 1;
+  const int64_t longest = ch.max_tokens ? std::min(ch.max_tokens, ch.num_tokens) : ch.num_tokens;
+  p.few = longest * p.G <= santa::kFewRows;
+  p.rows = p.few ? santa::kFewRows : santa::kManyRows;
+  p.tile_tokens = p.rows / p.G;
+  // whatever the lengths: n sequences with tokens have at most this many tiles
+  const int64_t n = std::min(p.B, ch.num_tokens);
+  p.tiles = (ch.num_tokens - n) / p.tile_tokens + n;
+  const int64_t keys = win ? std::min<int64_t>(kv->n_k, (int64_t)win->sinks + win->window + p.tile_tokens - 1) : kv->n_k;
+  p.step = p.few ? 128 : p.elem == 1 ? 32 : 64;
+  // about two workgroups per CU, none with fewer keys than its start costs
+  const int64_t groups = p.tiles * p.Hkv;
+  int64_t T = std::min<int64_t>(512 / groups, keys / (p.few ? 128 : 256));
+  if (g_opts.splits > 0) T = g_opts.splits;
+  p.T = (int)std::max<int64_t>(1, std::min<int64_t>(T, santa::kMaxSplits));
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off = align256(off + bytes);
+    return o;
+  };
+  take(santa::kErrBytes);  // the head that every layout shares (make_plan)
+  take((size_t)santa::kSyncRowsMax * santa::kSyncStride * 4);
+  if (p.T > 1) {
+    const size_t rows = (size_t)groups * p.T * p.rows;
+    p.off_stat = take(rows * 8);
+    p.off_part = take(rows * santa::kHeadDim * 4);
+  }
+  p.total = off;
+  return p;
 }
 
 santa::KvView make_view(const santa_kv_t *kv) {
@@ -295,6 +360,64 @@ santa_status_t common_checks(const void *q, const santa_kv_t *kv, const santa_sh
   if ((reinterpret_cast<uintptr_t>(q) & 15)) return fail(SANTA_ERR_UNSUPPORTED, "q must be 16-byte aligned");
   if (!std::isfinite(scale)) return fail(SANTA_ERR_INVALID_ARG, "scale must be finite");
   return SANTA_OK;
+}
+
+// santa_attend_chunk and santa_decode_window
+santa_status_t attend(const void *q, const santa_kv_t *kv, const santa_shape_t *sh, const santa_chunk_t *chunk,
+                      const santa_window_t *win, float scale, void *out, void *ws, size_t ws_bytes, void *stream) {
+  TimerScope timer_scope;
+  g_last_error.clear();
+  santa_chunk_t ch;
+  santa_status_t s = check_shape(sh);
+  if (s == SANTA_OK) s = check_kv(kv, sh, true, false);
+  if (s == SANTA_OK) s = check_chunk(chunk, sh, &ch);
+  if (s == SANTA_OK) s = check_window(win);
+  if (s != SANTA_OK) return s;
+  if (kv->k_new) return fail(SANTA_ERR_UNSUPPORTED, "k_new and v_new must be NULL: santa_rope_append stores new rows");
+  if (!q || !out) return fail(SANTA_ERR_INVALID_ARG, "q or out is NULL");
+  if (misaligned(q) || misaligned(out)) return fail(SANTA_ERR_UNSUPPORTED, "q and out must be 16-byte aligned");
+  if (!std::isfinite(scale)) return fail(SANTA_ERR_INVALID_ARG, "scale must be finite");
+  const santa::AttendPlan p = make_attend_plan(sh, kv, ch, win);
+  if (p.tiles * p.Hkv * std::max(p.T, p.rows) > INT32_MAX)
+    return fail(SANTA_ERR_UNSUPPORTED, "too many tokens times KV heads for one launch");
+  s = check_ws(p.total, ws, ws_bytes);
+  if (s != SANTA_OK) return s;
+  santa::AttendArgs a{};
+  a.kv = make_view(kv);
+  a.ch = santa::ChunkView{ch.q_start, sh->batch, ch.num_tokens};
+  a.q = q;
+  a.out = out;
+  a.stat = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.off_stat);
+  a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + p.off_part);
+  a.Hq = p.Hq;
+  a.Hkv = p.Hkv;
+  a.G = p.G;
+  a.tile_tokens = p.tile_tokens;
+  a.T = p.T;
+  a.step = p.step;
+  a.tiles = p.tiles;
+  a.window = win ? win->window : 0;
+  a.sinks = win ? win->sinks : 0;
+  a.scale_log2 = log2_scale(scale);
+  return hip_status(santa::launch_attend(p, a, static_cast<hipStream_t>(stream)));
+}
+
+// Turns per position of pair i, before any whole turns are left out.
+double rope_turns(const santa_rope_params_t &r, int i) {
+  const double pi2 = 6.283185307179586476925, R = r.rotary_dim;
+  const double theta = r.scaling == SANTA_ROPE_BASE ? r.theta * std::pow(r.factor, R / (R - 2)) : r.theta;
+  const double f = std::pow(theta, -2.0 * i / R);
+  double keep = 1.0;  // share of the unscaled frequency
+  if (r.scaling == SANTA_ROPE_LINEAR) keep = 0.0;
+  if (r.scaling == SANTA_ROPE_BANDS) keep = (r.original_len * f / pi2 - r.low) / (r.high - r.low);
+  if (r.scaling == SANTA_ROPE_RAMP) {
+    auto pair = [&](double turns) { return R * std::log(r.original_len / (pi2 * turns)) / (2.0 * std::log(r.theta)); };
+    const double lo = std::max(0.0, std::floor(pair(r.high))), hi = std::min(R - 1.0, std::ceil(pair(r.low)));
+    keep = 1.0 - (i - lo) / std::max(hi - lo, 0.001);
+  }
+  keep = std::min(1.0, std::max(0.0, keep));
+  const bool scaled = r.scaling != SANTA_ROPE_PLAIN && r.scaling != SANTA_ROPE_BASE;
+  return (scaled ? f * keep + f / r.factor * (1.0 - keep) : f) / pi2;
 }
 
 santa_status_t sampled(const void *q, const santa_kv_t *kv, const santa_shape_t *sh, float scale,
@@ -525,6 +648,111 @@ santa_status_t santa_decode_flash(const void *q, const santa_kv_t *kv, const san
   return hip_status(santa::launch_fused_flash(p, make_view(kv), q, log2_scale(scale), ilog2(tile),
                                               S_tile, u, idx_out, out, static_cast<char *>(ws),
                                               static_cast<hipStream_t>(stream), rows));
+}
+
+santa_status_t santa_rope_init(const santa_rope_params_t *params, santa_rope_t *rope) {
+  g_last_error.clear();
+  if (!params || !rope) return fail(SANTA_ERR_INVALID_ARG, "params or rope is NULL");
+  const santa_rope_params_t &r = *params;
+  if (r.rotary_dim < 16 || r.rotary_dim > santa::kHeadDim || r.rotary_dim % 16)
+    return fail(SANTA_ERR_UNSUPPORTED, "rotary_dim must be a multiple of 16 in [16, 128]");
+  if (r.interleaved != 0 && r.interleaved != 1) return fail(SANTA_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  if (!(r.theta > 1.0) || !std::isfinite(r.theta)) return fail(SANTA_ERR_INVALID_ARG, "theta must be > 1");
+  if (r.scaling < SANTA_ROPE_PLAIN || r.scaling > SANTA_ROPE_RAMP)
+    return fail(SANTA_ERR_INVALID_ARG, "scaling must be a santa_rope_scaling_t");
+  if (r.scaling != SANTA_ROPE_PLAIN && (!(r.factor > 0.0) || !std::isfinite(r.factor)))
+    return fail(SANTA_ERR_INVALID_ARG, "factor must be > 0");
+  if (r.scaling == SANTA_ROPE_BANDS || r.scaling == SANTA_ROPE_RAMP) {
+    if (!(r.original_len > 0.0) || !std::isfinite(r.original_len))
+      return fail(SANTA_ERR_INVALID_ARG, "original_len must be > 0");
+    if (!(r.low > 0.0) || !(r.high > r.low) || !std::isfinite(r.high))
+      return fail(SANTA_ERR_INVALID_ARG, "low and high must satisfy 0 < low < high");
+  }
+  if (!std::isfinite(r.gain)) return fail(SANTA_ERR_INVALID_ARG, "gain must be finite");
+  *rope = santa_rope_t{};
+  rope->rotary_dim = r.rotary_dim;
+  rope->interleaved = r.interleaved;
+  rope->gain = (float)(r.gain != 0.0 ? r.gain
+                       : r.scaling == SANTA_ROPE_RAMP && r.factor > 1.0 ? 0.1 * std::log(r.factor) + 1.0 : 1.0);
+  for (int i = 0; i < r.rotary_dim / 2; ++i) {
+    const double turns = rope_turns(r, i);
+    // (a fraction that rounds to a whole turn is one of 0: ldexp of it is 2^64)
+    const double x = std::ldexp(turns - std::floor(turns), 64);
+    rope->step[i] = x < 18446744073709551616.0 ? (uint64_t)x : 0;
+  }
+  return SANTA_OK;
+}
+
+santa_status_t santa_rope_append(const santa_rows_t *rows, const santa_kv_t *kv, const santa_shape_t *shape,
+                                 const santa_chunk_t *chunk, const santa_rope_t *rope, void *q_out, void *stream) {
+  TimerScope timer_scope;
+  g_last_error.clear();
+  santa_chunk_t ch;
+  santa_status_t s = check_shape(shape);
+  if (s == SANTA_OK) s = check_kv(kv, shape, true, false);
+  if (s == SANTA_OK) s = check_chunk(chunk, shape, &ch);
+  if (s != SANTA_OK) return s;
+  if (!rows || !rows->k || !rows->v) return fail(SANTA_ERR_INVALID_ARG, "rows, rows->k or rows->v is NULL");
+  if (!rows->q != !q_out) return fail(SANTA_ERR_INVALID_ARG, "rows->q and q_out go together");
+  if (!rope && rows->q) return fail(SANTA_ERR_INVALID_ARG, "without rope there is nothing to do for q: pass NULL");
+  if (kv->k_new) return fail(SANTA_ERR_INVALID_ARG, "kv->k_new and kv->v_new must be NULL (rows holds the new rows)");
+  if (rope && (rope->rotary_dim < 16 || rope->rotary_dim > santa::kHeadDim || rope->rotary_dim % 16))
+    return fail(SANTA_ERR_INVALID_ARG, "rope was not filled by santa_rope_init");
+  const int64_t a = shape->dtype == SANTA_BF16 ? 8 : 4;  // elements per 16 bytes
+  const int64_t qw = (int64_t)shape->num_q_heads * santa::kHeadDim, kw = (int64_t)shape->num_kv_heads * santa::kHeadDim;
+  if ((rows->q && rows->q_stride < qw) || rows->k_stride < kw || rows->v_stride < kw)
+    return fail(SANTA_ERR_INVALID_ARG, "row strides must hold all heads");
+  if (rows->q_stride % a || rows->k_stride % a || rows->v_stride % a || misaligned(rows->q) || misaligned(rows->k) ||
+      misaligned(rows->v) || misaligned(q_out))
+    return fail(SANTA_ERR_UNSUPPORTED, "rows and q_out must be 16-byte aligned");
+  if (q_out == rows->q && rows->q && rows->q_stride != qw)
+    return fail(SANTA_ERR_INVALID_ARG, "q_out may be q only if q is contiguous");
+  santa::RopeArgs r{};
+  r.kv = make_view(kv);
+  r.ch = santa::ChunkView{ch.q_start, shape->batch, ch.num_tokens};
+  r.q = rows->q;
+  r.k = rows->k;
+  r.v = rows->v;
+  r.q_st = rows->q_stride;
+  r.k_st = rows->k_stride;
+  r.v_st = rows->v_stride;
+  r.q_out = q_out;
+  r.positions = rows->positions;
+  r.Hq = rows->q ? shape->num_q_heads : 0;
+  r.Hkv = shape->num_kv_heads;
+  if (rope) {
+    r.rotary = rope->rotary_dim;
+    r.interleaved = rope->interleaved;
+    r.gain = rope->gain;
+    std::copy(rope->step, rope->step + santa::kHeadDim / 2, r.step);
+  }
+  return hip_status(santa::launch_rope(r, shape->dtype, kv->kv_dtype == SANTA_KV_FP8_E4M3 ? 2 : shape->dtype == SANTA_BF16 ? 0 : 1,
+                                       static_cast<hipStream_t>(stream)));
+}
+
+size_t santa_attend_workspace_size(const santa_shape_t *shape, const santa_kv_t *kv, const santa_chunk_t *chunk,
+                                   const santa_window_t *window) {
+  santa_chunk_t ch;
+  if (check_shape(shape) != SANTA_OK || !kv || kv->n_k < 1 || check_chunk(chunk, shape, &ch) != SANTA_OK ||
+      check_window(window) != SANTA_OK)
+    return 0;
+  return make_attend_plan(shape, kv, ch, window).total;
+}
+
+santa_status_t santa_attend_chunk(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,
+                                  const santa_chunk_t *chunk, const santa_window_t *window, float scale, void *out,
+                                  void *ws, size_t ws_bytes, void *stream) {
+  return attend(q, kv, shape, chunk, window, scale, out, ws, ws_bytes, stream);
+}
+
+santa_status_t santa_decode_window(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,
+                                   const santa_window_t *window, float scale, void *out, void *ws, size_t ws_bytes,
+                                   void *stream) {
+  if (!window) {
+    TimerScope timer_scope;
+    return fail(SANTA_ERR_INVALID_ARG, "window is NULL");
+  }
+  return attend(q, kv, shape, nullptr, window, scale, out, ws, ws_bytes, stream);
 }
 
 santa_status_t santa_stream_read(const void *buf, size_t bytes, uint32_t *sink, void *stream) {

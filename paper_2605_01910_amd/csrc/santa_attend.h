@@ -1,0 +1,618 @@
+// santa_attend.h -- attention of a chunk of new tokens over the KV cache, causal
+// or with a sliding window and sinks (santa_attend_chunk, santa_decode_window).
+//
+// Rows.  The G query heads of a KV head attend over the same keys, so a tile's
+// rows are (token, head) pairs, row r = token r / G, head r % G: a key row read
+// once serves the whole group, and eight single-token rows fill a matrix tile
+// as well as a long chunk does.
+//
+// Scores are computed transposed, S^T = K Q^T, with 32 keys as the matrix
+// instruction's rows and 32 query rows as its columns: lane l then holds 16
+// keys of query row l % 32 (keys 8 a + 4 (l / 32) + j in accumulator 4 a + j),
+// so the running maximum and sum of a row need one exchange between two lanes.
+// The output is transposed too, O^T += V^T P^T, and the weights are its right
+// operand as they stand: an instruction sums over 16 keys, and which of them a
+// lane holds is free as long as both operands agree, so lane l takes the keys
+// it scored and V's operand is read from LDS to match (a transposing read for
+// 16-bit elements).  Rescaling a row of O^T is one multiplication per register.
+//
+// Keys.  The keys that a tile's tokens can see are the sinks [0, n0) and a run
+// that ends at its last token; they are numbered v = 0 .. nv - 1 without the
+// gap between, so no tile is spent on hidden keys and rows outside are never
+// touched (their pages may have been freed).
+#pragma once
+
+#include "santa_chunk.h"
+#include "santa_device.h"
+#include "santa_kernels.h"
+#include "santa_tiles.h"
+
+namespace santa {
+
+typedef __bf16 abf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 abf16x2 __attribute__((ext_vector_type(2)));
+typedef short as16x4 __attribute__((ext_vector_type(4)));
+typedef float af32x16 __attribute__((ext_vector_type(16)));
+
+// Element type in LDS: FP8 codes are widened (exactly) on the way in.
+template <typename E>
+using LE = QE<E>;
+
+// Visible keys of a tile: v < n0 is position v, v >= n0 position v + shift.
+struct KeyMap {
+  int n0, shift, nv;
+  __device__ __forceinline__ int pos(int v) const { return v < n0 ? v : v + shift; }
+};
+
+// Tokens at positions p_lo .. p_hi together see [0, sinks) and (p_lo - window, p_hi].
+__device__ __forceinline__ KeyMap key_map(int p_lo, int p_hi, int window, int sinks) {
+  const int lo = window ? max(0, p_lo - window + 1) : 0;
+  if (lo <= sinks) return KeyMap{0, 0, p_hi + 1};
+  return KeyMap{sinks, lo - sinks, sinks + p_hi + 1 - lo};
+}
+
+// What row r of a tile sees, in v: v < hi and (v >= lo or v < sv).
+struct RowSight {
+  int lo, hi, sv;
+};
+__device__ __forceinline__ RowSight row_sight(const KeyMap &km, int p, int window, int sinks) {
+  RowSight s;
+  const int first = window ? max(0, p - window + 1) : 0;  // the window's first position
+  s.hi = p < km.n0 + km.shift ? min(p + 1, km.n0) : p + 1 - km.shift;
+  s.lo = km.shift ? km.n0 + max(0, first - km.n0 - km.shift) : first;
+  s.sv = km.shift ? km.n0 : min(sinks, km.nv);
+  return s;
+}
+
+// 16-byte chunk c of LDS row `row` stands at chunk c ^ swizzle: the lanes of a
+// key read take one chunk of 32 rows, those of a value read four rows' (or,
+// 32-bit, two rows') same chunks; either way they spread over all banks.
+template <typename L>
+__device__ __forceinline__ int k_swz(int row) {
+  return row & 15;
+}
+template <typename L>
+__device__ __forceinline__ int v_swz(int row) {
+  return sizeof(L) == 2 ? (row & 3) << 2 : ((row >> 2) & 1) << 3;
+}
+template <typename L>
+constexpr int lds_row() {
+  return kHeadDim * (int)sizeof(L);
+}
+
+// Query rows as the right operand of S^T = K Q^T: lane l holds row l % 32,
+// features 16 s + 8 (l / 32) .. + 7 of step s.
+template <typename L>
+struct AQ;
+template <>
+struct AQ<uint16_t> {
+  abf16x8 f[8];
+};
+template <>
+struct AQ<float> {
+  float4 f[16];  // features 8 s + 4 (l / 32) .. + 3
+};
+
+// `neg`: the negated row (a negative scale becomes a positive one).
+__device__ __forceinline__ void load_rows(AQ<uint16_t> &q, const uint16_t *p, bool valid, bool neg) {
+  const int h = (threadIdx.x >> 5) & 1;
+  const uint32_t flip = neg ? 0x80008000u : 0u;
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (valid) w = *reinterpret_cast<const uint4 *>(p + 16 * s + 8 * h);
+    q.f[s] = __builtin_bit_cast(abf16x8, make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip));
+  }
+}
+__device__ __forceinline__ void load_rows(AQ<float> &q, const float *p, bool valid, bool neg) {
+  const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int s = 0; s < 16; ++s) {
+    float4 w = make_float4(0, 0, 0, 0);
+    if (valid) w = *reinterpret_cast<const float4 *>(p + 8 * s + 4 * h);
+    q.f[s] = neg ? make_float4(-w.x, -w.y, -w.z, -w.w) : w;
+  }
+}
+
+// Scores of keys [32 t, 32 t + 32) of the tile at K, raw (before the scale).
+__device__ __forceinline__ af32x16 score_block(const AQ<uint16_t> &q, const char *K, int t) {
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  const char *row = K + (32 * t + r) * lds_row<uint16_t>();
+  const int x = h ^ (r & 15);
+  af32x16 s = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const abf16x8 k = *reinterpret_cast<const abf16x8 *>(row + (((2 * i) ^ x) << 4));
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q.f[i], s, 0, 0, 0);
+  }
+  return s;
+}
+__device__ __forceinline__ af32x16 score_block(const AQ<float> &q, const char *K, int t) {
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  const char *row = K + (32 * t + r) * lds_row<float>();
+  const int x = h ^ (r & 15);
+  af32x16 s = {};
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float4 k = *reinterpret_cast<const float4 *>(row + (((2 * i) ^ x) << 4));
+    s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, q.f[i].x, s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, q.f[i].y, s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, q.f[i].z, s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, q.f[i].w, s, 0, 0, 0);
+  }
+  return s;
+}
+
+// The running state of 32 rows in a wave: maximum (raw score units, the same
+// on both lanes of a row), the lane's share of the sum, and O^T: feature
+// 32 n + 8 a + 4 (l / 32) + j of row l % 32 in o[n][4 a + j].
+struct RowState {
+  float m, l;
+  af32x16 o[4];
+};
+
+// Four keys' values as one operand half: features 32 n + l % 32 of keys
+// row .. row + 3 (row: a multiple of 4 that depends on l / 32).
+__device__ __forceinline__ as16x4 value_quad(const char *V, int row, int n) {
+  const int l = threadIdx.x & 15, g = (threadIdx.x >> 4) & 1, k = l >> 2;
+  const char *p = V + (row + k) * lds_row<uint16_t>() + (((4 * n + 2 * g + ((l & 3) >> 1)) ^ (k << 2)) << 4) +
+                  (l & 1) * 8;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) as16x4 *)(reinterpret_cast<const as16x4 *>(p)));
+}
+
+// Non-finite values stand apart: a key that some rows of the tile do not see
+// must not reach them as 0 * inf.  clean: the operand with those elements 0;
+// mark: 1 where the element is of the kind (0: +inf, 1: -inf, 2: NaN).
+__device__ __forceinline__ uint32_t nonfinite2(uint32_t w) {  // 0xffff halves where exponent is all ones
+  const uint32_t e = w & 0x7f807f80u;
+  return ((e & 0xffffu) == 0x7f80u ? 0xffffu : 0u) | ((e >> 16) == 0x7f80u ? 0xffff0000u : 0u);
+}
+__device__ __forceinline__ uint32_t mark2(uint32_t w, int kind) {
+  auto one = [&](uint32_t x) {
+    const bool inf = (x & 0x7fffu) == 0x7f80u, nan = (x & 0x7fffu) > 0x7f80u;
+    return (kind == 2 ? nan : inf && ((x >> 15) != 0) == (kind == 1)) ? 0x3f80u : 0u;
+  };
+  return one(w & 0xffffu) | one(w >> 16) << 16;
+}
+__device__ __forceinline__ float mark1(float x, int kind) {
+  const bool nan = x != x;
+  return (kind == 2 ? nan : x == (kind ? -kInf : kInf)) ? 1.0f : 0.0f;
+}
+__device__ __forceinline__ float mark_value(int kind) {
+  return kind == 0 ? kInf : kind == 1 ? -kInf : __builtin_nanf("");
+}
+
+// O^T += V^T P^T over keys [32 t, 32 t + 32) of the tile at V.  EDGE: some row
+// may not see some of the keys (their weights are 0).
+template <bool EDGE>
+__device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, uint16_t) {
+  const int h = (threadIdx.x >> 5) & 1;
+  abf16x8 pf[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pf[b][i] = (__bf16)p[8 * b + i];  // nearest even: 2^-9 of a weight, the sum keeps 32 bits
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    uint4 w[2];
+    uint32_t bad = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int row = 32 * t + 16 * b + 4 * h;
+      const as16x4 x = value_quad(V, row, n), y = value_quad(V, row + 8, n);
+      const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
+      w[b] = make_uint4(u.x, u.y, v.x, v.y);
+      if constexpr (EDGE)
+        bad |= nonfinite2(w[b].x) | nonfinite2(w[b].y) | nonfinite2(w[b].z) | nonfinite2(w[b].w);
+    }
+    if (EDGE && __any(bad != 0)) {
+#pragma unroll 1
+      for (int kind = 0; kind < 3; ++kind) {
+        af32x16 c = {};
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint4 mk = make_uint4(mark2(w[b].x, kind), mark2(w[b].y, kind), mark2(w[b].z, kind), mark2(w[b].w, kind));
+          c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, mk), pf[b], c, 0, 0, 0);
+        }
+        const float add = mark_value(kind);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[n][i] += c[i] > 0.0f ? add : 0.0f;
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        w[b] = make_uint4(w[b].x & ~nonfinite2(w[b].x), w[b].y & ~nonfinite2(w[b].y), w[b].z & ~nonfinite2(w[b].z),
+                          w[b].w & ~nonfinite2(w[b].w));
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, w[b]), pf[b], st.o[n], 0, 0, 0);
+  }
+}
+template <bool EDGE>
+__device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, float) {
+  const int lane = threadIdx.x & 63, d = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const char *col = V + (32 * t + 4 * h) * lds_row<float>() + (((8 * n + (d >> 2)) ^ (h << 3)) << 4) + (d & 3) * 4;
+    float w[16];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      w[i] = *reinterpret_cast<const float *>(col + (8 * (i >> 2) + (i & 3)) * lds_row<float>());
+      if constexpr (EDGE) bad |= !(fabsf(w[i]) < kInf);
+    }
+    if (EDGE && __any(bad)) {
+#pragma unroll 1
+      for (int kind = 0; kind < 3; ++kind) {
+        af32x16 c = {};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(mark1(w[i], kind), p[i], c, 0, 0, 0);
+        const float add = mark_value(kind);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[n][i] += c[i] > 0.0f ? add : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = fabsf(w[i]) < kInf ? w[i] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st.o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], p[i], st.o[n], 0, 0, 0);
+  }
+}
+
+// One step of the online softmax over NB blocks of 32 keys whose K and V rows
+// are in LDS; v0: the first key's number.
+template <typename L, int NB, bool EDGE>
+__device__ __forceinline__ void attend_step(RowState &st, const AQ<L> &q, const char *K, const char *V, int v0,
+                                            const RowSight &rs, float c) {
+  const int h = (threadIdx.x >> 5) & 1;
+  af32x16 s[NB];
+  float tm = -kInf;
+#pragma unroll
+  for (int t = 0; t < NB; ++t) {
+    s[t] = score_block(q, K, t);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if constexpr (EDGE) {
+        const int v = v0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3);
+        if (!(v < rs.hi && (v >= rs.lo || v < rs.sv))) s[t][i] = -kInf;
+      }
+      tm = fmaxf(tm, s[t][i]);
+    }
+  }
+  tm = xor32_max(tm);
+  const float mn = fmaxf(st.m, tm);
+  const float mc = mn == -kInf ? 0.0f : mn * c;  // nothing visible yet: every weight is 0
+  if (__any(mn > st.m)) {
+    const float f = fast_exp2(fmaf(st.m, c, -mc));
+    st.l *= f;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.o[n][i] *= f;
+    st.m = mn;
+  }
+#pragma unroll
+  for (int t = 0; t < NB; ++t) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[t][i] = fast_exp2(fmaf(s[t][i], c, -mc));
+      st.l += s[t][i];
+    }
+    add_values<EDGE>(st, s[t], V, t, L{});
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Cache rows into LDS
+// ---------------------------------------------------------------------------
+// KEYS rows of K and V, keys v0 .. of the tile, by a team of TEAM lanes (`tl`:
+// this lane's number); rows past `end` are zeros.
+template <typename E, bool PAGED, int KEYS, int TEAM>
+__device__ __forceinline__ void stage_rows(const KvView &kv, int b, int kvh, const KeyMap &km, int v0, int end,
+                                           int tl, char *K, char *V) {
+  using L = LE<E>;
+  constexpr int CPR = kHeadDim * (int)sizeof(E) / 16;  // 16-byte chunks of a cache row
+  constexpr int N = KEYS * CPR / TEAM;
+  static_assert(KEYS * CPR % TEAM == 0, "whole chunks per lane");
+  const char *kb = static_cast<const char *>(kv.k), *vb = static_cast<const char *>(kv.v);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int i = n * TEAM + tl, row = i / CPR, ch = i % CPR, v = v0 + row;
+    uint4 kw = make_uint4(0, 0, 0, 0), vw = make_uint4(0, 0, 0, 0);
+    if (v < end) {
+      const int64_t off = row_offset<PAGED>(kv, b, kvh, km.pos(v)) * (int64_t)sizeof(E) + ch * 16;
+      kw = *reinterpret_cast<const uint4 *>(kb + off);
+      vw = *reinterpret_cast<const uint4 *>(vb + off);
+    }
+    char *kd = K + row * lds_row<L>(), *vd = V + row * lds_row<L>();
+    const int kx = k_swz<L>(row), vx = v_swz<L>(row);
+    if constexpr (sizeof(E) == 1) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const Chunk<uint8_t> a{half ? make_uint2(kw.z, kw.w) : make_uint2(kw.x, kw.y)};
+        const Chunk<uint8_t> c{half ? make_uint2(vw.z, vw.w) : make_uint2(vw.x, vw.y)};
+        *reinterpret_cast<uint4 *>(kd + (((2 * ch + half) ^ kx) << 4)) = a.to_bf16();
+        *reinterpret_cast<uint4 *>(vd + (((2 * ch + half) ^ vx) << 4)) = c.to_bf16();
+      }
+    } else {
+      *reinterpret_cast<uint4 *>(kd + ((ch ^ kx) << 4)) = kw;
+      *reinterpret_cast<uint4 *>(vd + ((ch ^ vx) << 4)) = vw;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles
+// ---------------------------------------------------------------------------
+// A workgroup's tile and key range.  Blocks are numbered KV head fastest (with
+// 8 KV heads each XCD works on one head's keys), then split, then tile from
+// the batch's last to its first: in a chunk the later tiles see more keys.
+struct Work {
+  TileAt at;
+  int kvh, t, rows, p_lo;  // rows: valid ones; p_lo: position of the tile's first token
+  int v_begin, v_end;
+  KeyMap km;
+  int64_t out_row;         // first row of the tile's partial results
+  bool any;                // the tile exists
+};
+__device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile) {
+  Work w;
+  const int64_t id = blockIdx.x;
+  w.kvh = (int)(id % a.Hkv);
+  w.t = (int)(id / a.Hkv % a.T);
+  const int64_t x = a.tiles - 1 - id / a.Hkv / a.T;
+  w.at = find_tile(a.ch, x, a.tile_tokens);
+  w.any = w.at.b < a.ch.B;
+  w.out_row = ((x * a.Hkv + w.kvh) * a.T + w.t) * rows_per_tile;
+  if (!w.any) return w;
+  const int L = seq_len(a.kv, w.at.b), n = min(a.tile_tokens, w.at.count - w.at.i0);
+  w.rows = n * a.G;
+  w.p_lo = L - w.at.count + w.at.i0;
+  // (a chunk longer than its context: tokens before position 0 see nothing)
+  w.km = w.p_lo + n - 1 < 0 ? KeyMap{0, 0, 0} : key_map(max(w.p_lo, 0), w.p_lo + n - 1, a.window, a.sinks);
+  const int len = ((w.km.nv + a.T - 1) / a.T + a.step - 1) / a.step * a.step;
+  w.v_begin = min(w.t * len, w.km.nv);
+  w.v_end = min(w.v_begin + len, w.km.nv);
+  return w;
+}
+
+// Row r of the tile: its query row, and what it sees.  Rows past the last see
+// what the last one sees (their results are dropped).
+struct Row {
+  bool valid;
+  int64_t at;  // elements into q and out
+  RowSight see;
+};
+__device__ __forceinline__ Row tile_row(const AttendArgs &a, const Work &w, int r) {
+  Row x;
+  x.valid = r < w.rows;
+  const int rr = min(r, w.rows - 1), i = rr / a.G;
+  x.at = ((int64_t)(w.at.first + w.at.i0 + i) * a.Hq + w.kvh * a.G + rr % a.G) * kHeadDim;
+  const int p = w.p_lo + i;
+  x.see = p < 0 ? RowSight{0, 0, 0} : row_sight(w.km, p, a.window, a.sinks);
+  return x;
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const abf16x2 v = {(__bf16)a, (__bf16)b};  // the one rounding of an output
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ void store4(uint16_t *p, float4 v) {
+  *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+}
+__device__ __forceinline__ void store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
+
+// Scale of the scores as a non-negative factor and the sign that goes into the
+// queries; with a factor of 0 the queries are zeroed instead.
+struct Scale {
+  float c;
+  bool neg, zero;
+};
+template <typename E>
+__device__ __forceinline__ Scale score_scale(const AttendArgs &a, float2 sc) {
+  const float c = a.scale_log2 * sc.x;
+  return c == 0.0f ? Scale{1.0f, false, true} : Scale{fabsf(c), c < 0.0f, false};
+}
+
+// Many rows: 128 rows, 32 per wave; K and V tiles of KEYS keys shared by the
+// four waves.
+template <typename E>
+constexpr int many_keys() {
+  return sizeof(E) == 4 ? 32 : 64;
+}
+template <typename E, bool PAGED>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttendArgs a) {
+  using L = LE<E>;
+  constexpr int KEYS = many_keys<E>(), NB = KEYS / 32;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  char *K = lds, *V = lds + KEYS * lds_row<L>();
+  const Work w = find_work(a, kManyRows);
+  if (!w.any) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = 32 * wave + (lane & 31), h = lane >> 5;
+  const Row row = tile_row(a, w, r);
+  const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
+  const Scale scale = score_scale<E>(a, sc);
+  AQ<L> q;
+  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
+  // what all of the wave's rows see, and what any of them does
+  const bool live = 32 * wave < w.rows;
+  const Row first = tile_row(a, w, 32 * wave), last = tile_row(a, w, min(32 * wave + 31, w.rows - 1));
+
+  RowState st;
+  st.m = -kInf;
+  st.l = 0.0f;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
+  for (int v0 = w.v_begin; v0 < w.v_end; v0 += KEYS) {
+    const int v1 = min(v0 + KEYS, w.v_end);
+    __syncthreads();
+    stage_rows<E, PAGED, KEYS, kThreads>(a.kv, w.at.b, w.kvh, w.km, v0, w.v_end, tid, K, V);
+    __syncthreads();
+    if (!live || v0 >= last.see.hi || (v1 <= first.see.lo && v0 >= first.see.sv)) continue;
+    const bool whole = v0 + KEYS <= min(first.see.hi, w.v_end) && (v0 >= last.see.lo || v0 + KEYS <= last.see.sv);
+    RowSight see = row.see;
+    see.hi = min(see.hi, w.v_end);
+    if (whole) attend_step<L, NB, false>(st, q, K, V, v0, see, scale.c);
+    else attend_step<L, NB, true>(st, q, K, V, v0, see, scale.c);
+  }
+
+  const float l = xor32_sum(st.l);
+  if (!row.valid) return;
+  if (a.T == 1) {
+    const float f = l > 0.0f || l != l ? sc.y / l : 0.0f;  // a row that sees nothing is zero
+    L *out = static_cast<L *>(a.out) + row.at;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        store4(out + 32 * n + 8 * g + 4 * h, make_float4(st.o[n][4 * g] * f, st.o[n][4 * g + 1] * f,
+                                                         st.o[n][4 * g + 2] * f, st.o[n][4 * g + 3] * f));
+  } else {
+    const int64_t at = w.out_row + r;
+    if (h == 0) a.stat[at] = make_float2(st.m == -kInf ? -kInf : st.m * scale.c, l);
+    if (st.m == -kInf) return;  // (nothing seen here: the sum 0 says so)
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4 *>(a.part + at * kHeadDim + 32 * n + 8 * g + 4 * h) =
+            make_float4(st.o[n][4 * g], st.o[n][4 * g + 1], st.o[n][4 * g + 2], st.o[n][4 * g + 3]);
+  }
+}
+
+// Few rows: up to 32, the same for all four waves, which take 32 keys in turn
+// and join their results through LDS at the end.
+template <typename E, bool PAGED>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) void k_attend_few(AttendArgs a) {
+  using L = LE<E>;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ float wm[4][kFewRows], wl[4][kFewRows];
+  const Work w = find_work(a, kFewRows);
+  if (!w.any) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 31, h = lane >> 5;
+  char *K = lds + wave * 64 * lds_row<L>(), *V = K + 32 * lds_row<L>();
+  const Row row = tile_row(a, w, r);
+  const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
+  const Scale scale = score_scale<E>(a, sc);
+  AQ<L> q;
+  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
+  const Row first = tile_row(a, w, 0), last = tile_row(a, w, w.rows - 1);
+  RowSight see = row.see;
+  see.hi = min(see.hi, w.v_end);
+
+  RowState st;
+  st.m = -kInf;
+  st.l = 0.0f;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
+  for (int v0 = w.v_begin + 32 * wave; v0 < w.v_end; v0 += 128) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    stage_rows<E, PAGED, 32, 64>(a.kv, w.at.b, w.kvh, w.km, v0, w.v_end, lane, K, V);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const bool whole = v0 + 32 <= min(first.see.hi, w.v_end) && (v0 >= last.see.lo || v0 + 32 <= last.see.sv);
+    if (whole) attend_step<L, 1, false>(st, q, K, V, v0, see, scale.c);
+    else attend_step<L, 1, true>(st, q, K, V, v0, see, scale.c);
+  }
+
+  // join the waves: out = sum_w 2^(m_w - m) O_w / sum_w 2^(m_w - m) l_w
+  const float l = xor32_sum(st.l);
+  if (h == 0) {
+    wm[wave][r] = st.m == -kInf ? -kInf : st.m * scale.c;
+    wl[wave][r] = l;
+  }
+  __syncthreads();  // (also: every wave is done with its tile's memory)
+  float m = -kInf;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = fmaxf(m, wm[i][r]);
+  const float f = st.m == -kInf ? 0.0f : fast_exp2(st.m * scale.c - m);
+  float4 *part = reinterpret_cast<float4 *>(lds);  // [wave][32 quads of features][32 rows]
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      part[(wave * 32 + 8 * n + 2 * g + h) * 32 + r] = make_float4(st.o[n][4 * g] * f, st.o[n][4 * g + 1] * f,
+                                                                   st.o[n][4 * g + 2] * f, st.o[n][4 * g + 3] * f);
+  __syncthreads();
+  const int r2 = tid & 31, d0 = tid >> 5;  // row, and its features 16 d0 .. + 15
+  if (r2 >= w.rows) return;
+  float mm = -kInf, ll = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) mm = fmaxf(mm, wm[i][r2]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ll += wm[i][r2] == -kInf ? 0.0f : fast_exp2(wm[i][r2] - mm) * wl[i][r2];
+  const int64_t at = w.out_row + r2;
+  const float g = a.T > 1 ? 1.0f : ll > 0.0f || ll != ll ? sc.y / ll : 0.0f;
+  const Row row2 = tile_row(a, w, r2);
+  if (a.T > 1 && d0 == 0) a.stat[at] = make_float2(mm, ll);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float4 x = make_float4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 y = part[(i * 32 + 4 * d0 + k) * 32 + r2];
+      x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+    }
+    x = make_float4(x.x * g, x.y * g, x.z * g, x.w * g);
+    if (a.T > 1) *reinterpret_cast<float4 *>(a.part + at * kHeadDim + 16 * d0 + 4 * k) = x;
+    else store4(static_cast<L *>(a.out) + row2.at + 16 * d0 + 4 * k, x);
+  }
+}
+
+// Joins the splits' partial results, a wave per (KV head, row of a tile).
+template <typename E, int ROWS>
+__global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
+  using L = LE<E>;
+  const int lane = threadIdx.x & 63;
+  const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int r = (int)(id % ROWS), kvh = (int)(id / ROWS % a.Hkv);
+  const int64_t x = id / ROWS / a.Hkv;
+  if (x >= a.tiles) return;
+  const TileAt at = find_tile(a.ch, x, a.tile_tokens);
+  if (at.b >= a.ch.B) return;
+  const int i = r / a.G;
+  if (i >= min(a.tile_tokens, at.count - at.i0) || i >= a.tile_tokens) return;
+  const int64_t base = (x * a.Hkv + kvh) * a.T * ROWS + r;
+  float m = -kInf;
+  for (int t = 0; t < a.T; ++t) m = fmaxf(m, a.stat[base + (int64_t)t * ROWS].x);
+  float2 o = make_float2(0, 0);
+  float l = 0.0f;
+  for (int t = 0; t < a.T; ++t) {
+    const float2 s = a.stat[base + (int64_t)t * ROWS];
+    if (s.x == -kInf) continue;  // the split holds no key that the row sees
+    const float f = fast_exp2(s.x - m);
+    const float2 y = reinterpret_cast<const float2 *>(a.part + (base + (int64_t)t * ROWS) * kHeadDim)[lane];
+    l = fmaf(f, s.y, l);
+    o = make_float2(fmaf(f, y.x, o.x), fmaf(f, y.y, o.y));
+  }
+  const float g = l > 0.0f || l != l ? kv_scales<E>(a.kv, at.b, kvh, a.Hkv).y / l : 0.0f;
+  L *out = static_cast<L *>(a.out) + ((int64_t)(at.first + at.i0 + i) * a.Hq + kvh * a.G + r % a.G) * kHeadDim;
+  if constexpr (sizeof(L) == 2) reinterpret_cast<uint32_t *>(out)[lane] = pack2(o.x * g, o.y * g);
+  else reinterpret_cast<float2 *>(out)[lane] = make_float2(o.x * g, o.y * g);
+}
+
+template <typename E>
+constexpr size_t attend_lds(bool few) {
+  return few ? (size_t)4 * 64 * lds_row<LE<E>>() : (size_t)2 * many_keys<E>() * lds_row<LE<E>>();
+}
+
+template <typename E>
+hipError_t launch_attend_e(const AttendPlan &p, const AttendArgs &a, hipStream_t st) {
+  const CallTimer tm = call_timer();
+  void *params[] = {const_cast<AttendArgs *>(&a)};
+  const bool paged = a.kv.bt != nullptr;
+  const void *fn = p.few ? (paged ? (const void *)k_attend_few<E, true> : (const void *)k_attend_few<E, false>)
+                         : (paged ? (const void *)k_attend_many<E, true> : (const void *)k_attend_many<E, false>);
+  hipError_t e = hipExtLaunchKernel(fn, dim3((unsigned)(p.tiles * p.Hkv * p.T)), dim3(kThreads), params,
+                                    attend_lds<E>(p.few), st, tm.start, p.T > 1 ? nullptr : tm.stop, 0);
+  if (e != hipSuccess || p.T == 1) return e;
+  const void *mf = p.few ? (const void *)k_attend_merge<E, kFewRows> : (const void *)k_attend_merge<E, kManyRows>;
+  return hipExtLaunchKernel(mf, dim3((unsigned)(p.tiles * p.Hkv * p.rows / (kThreads / 64))), dim3(kThreads), params,
+                            0, st, nullptr, tm.stop, 0);
+}
+
+}  // namespace santa

@@ -1,0 +1,131 @@
+// santa_chunk.h -- ragged batches of new tokens (santa_chunk_t) as the kernels
+// of santa_rope_append and santa_attend_chunk see them, and their launchers.
+#pragma once
+
+#include <hip/hip_ext.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "santa.h"
+#include "santa_plan.h"
+
+namespace santa {
+
+// New tokens of a batch: sequence b's are rows [q_start[b], q_start[b + 1]) of
+// the row buffers and take the last positions of its ctx_len[b] keys.
+struct ChunkView {
+  const int32_t *q_start;  // [B + 1]; null: one token per sequence, row b
+  int32_t B, tokens;       // sequences; rows of the buffers
+};
+
+struct RopeArgs {
+  KvView kv;
+  ChunkView ch;
+  const void *q, *k, *v;
+  int64_t q_st, k_st, v_st;  // elements from one token's row to the next
+  void *q_out;
+  const int32_t *positions;  // nullable: the positions to rotate by, per token
+  int32_t Hq, Hkv;           // Hq = 0: no queries
+  int32_t rotary, interleaved;
+  float gain;
+  uint64_t step[kHeadDim / 2];  // 2^64 * fraction of a turn per position, by pair
+};
+
+// dtype: 0 bfloat16, 1 float32 rows; elem: as Plan::elem
+hipError_t launch_rope(const RopeArgs &a, int dtype, int elem, hipStream_t st);
+
+// Launch plan of the chunk's attention: a pure function of (shape, n_k, chunk,
+// window, options), so santa_attend_workspace_size and the calls agree.
+struct AttendPlan {
+  int B, Hq, Hkv, G, dtype, elem;
+  int few;            // 1: tiles of up to kFewRows rows whose waves share out the keys
+  int rows;           // query rows (tokens x group) per tile
+  int tile_tokens;    // tokens per tile: rows / G
+  int64_t tiles;      // upper bound of the batch's tiles per KV head
+  int T;              // key splits per tile; 1: no partial results
+  int step;           // split lengths are multiples of this
+  size_t off_stat;    // float2 [tiles * Hkv * T * rows] (max in log2 units, sum)
+  size_t off_part;    // float [tiles * Hkv * T * rows * 128]
+  size_t total;
+};
+
+struct AttendArgs {
+  KvView kv;
+  ChunkView ch;
+  const void *q;
+  void *out;
+  float2 *stat;
+  float *part;
+  int32_t Hq, Hkv, G, tile_tokens, T, step;
+  int64_t tiles;
+  int32_t window, sinks;  // window 0: every earlier key
+  float scale_log2;
+};
+
+constexpr int kFewRows = 32;    // rows of a "few" tile: one matrix instruction's columns
+constexpr int kManyRows = 128;  // rows of a full tile: 32 per wave
+
+hipError_t launch_attend(const AttendPlan &p, const AttendArgs &a, hipStream_t st);
+template <typename E>
+hipError_t launch_attend_e(const AttendPlan &p, const AttendArgs &a, hipStream_t st);
+
+#ifdef __HIPCC__
+// The sequence of token t and the range of its tokens, by the whole wave: 64
+// ends per load, no search chain.  b = B when no sequence holds the token.
+struct TokenAt {
+  int b, first, count;
+};
+__device__ __forceinline__ TokenAt find_token(const ChunkView &c, int t) {
+  if (!c.q_start) return t < c.B ? TokenAt{t, t, 1} : TokenAt{c.B, 0, 0};
+  const int lane = threadIdx.x & 63;
+  int b = 0;
+  for (int base = 0; base < c.B; base += 64) {
+    const int i = base + lane;
+    const bool before = i < c.B && c.q_start[i + 1] <= t;
+    const int n = __popcll(__ballot(before));
+    b = base + n;
+    if (n < 64) break;
+  }
+  if (b >= c.B) return TokenAt{c.B, 0, 0};
+  const int first = c.q_start[b], end = c.q_start[b + 1];
+  return TokenAt{b, first, end - first};
+}
+
+// Tile x of the batch (every sequence's tokens in tiles of `tt`, sequence by
+// sequence): its sequence, its first token in the chunk and the chunk's range.
+// b = B past the last tile.  Ends outside [0, tokens] are clamped, so a tile
+// never names a row outside the buffers.
+struct TileAt {
+  int b, first, count, i0;
+};
+__device__ __forceinline__ TileAt find_tile(const ChunkView &c, int64_t x, int tt) {
+  if (!c.q_start) return x < c.B ? TileAt{(int)x, (int)x, 1, 0} : TileAt{c.B, 0, 0, 0};
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int base = 0; base < c.B; base += 64) {
+    const int i = base + lane;
+    int s = 0, e = 0;
+    if (i < c.B) {
+      s = min(max(c.q_start[i], 0), c.tokens);
+      e = min(max(c.q_start[i + 1], s), c.tokens);
+    }
+    const int n = (e - s + tt - 1) / tt;
+    int incl = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    const unsigned long long hit = __ballot(before + incl > x);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int fs = __shfl(s, l), fe = __shfl(e, l), fi = __shfl(incl - n, l);
+      return TileAt{base + l, fs, fe - fs, (int)(x - before - fi) * tt};
+    }
+    before += __shfl(incl, 63);
+  }
+  return TileAt{c.B, 0, 0, 0};
+}
+#endif
+
+}  // namespace santa

@@ -4,6 +4,7 @@
 // santa_dense.h.
 #include <mutex>
 
+#include "santa_chunk.h"
 #include "santa_fused.h"
 
 namespace santa {
@@ -126,6 +127,11 @@ hipError_t launch_fused_bernoulli(const Plan &p, const KvView &kv, const KtView 
                                    out, ws, st);
     }
   });
+}
+
+hipError_t launch_attend(const AttendPlan &p, const AttendArgs &a, hipStream_t st) {
+  if (p.elem == 2) return launch_attend_e<uint8_t>(p, a, st);
+  return p.elem == 0 ? launch_attend_e<uint16_t>(p, a, st) : launch_attend_e<float>(p, a, st);
 }
 
 }  // namespace santa

@@ -26,6 +26,10 @@ SANTA_KV_AS_Q, SANTA_KV_FP8_E4M3 = 0, 1
  SANTA_KIND_FLASH, SANTA_KIND_IID) = range(6)
 (SANTA_PATH_AUTO, SANTA_PATH_ONE_LAUNCH, SANTA_PATH_TWO_LAUNCH, SANTA_PATH_MULTI,
  SANTA_PATH_SCHEDULED) = range(5)
+(SANTA_ROPE_PLAIN, SANTA_ROPE_LINEAR, SANTA_ROPE_BASE, SANTA_ROPE_BANDS,
+ SANTA_ROPE_RAMP) = range(5)
+ROPE_SCALINGS = {"none": SANTA_ROPE_PLAIN, "linear": SANTA_ROPE_LINEAR, "base": SANTA_ROPE_BASE,
+                 "bands": SANTA_ROPE_BANDS, "ramp": SANTA_ROPE_RAMP}
 PATHS = {"auto": SANTA_PATH_AUTO, "one": SANTA_PATH_ONE_LAUNCH, "two": SANTA_PATH_TWO_LAUNCH,
          "multi": SANTA_PATH_MULTI, "rows": SANTA_PATH_SCHEDULED}
 
@@ -34,7 +38,9 @@ EXPORTS = ("santa_workspace_size", "santa_workspace_init", "santa_decode_dense",
            "santa_decode_systematic", "santa_decode_stratified", "santa_decode_bernoulli_qk",
            "santa_decode_iid", "santa_decode_flash", "santa_stream_read", "santa_time_next_call",
            "santa_set_options", "santa_get_options", "santa_plan_info",
-           "santa_decode_stratified_noalloc", "santa_status_string", "santa_last_error")
+           "santa_decode_stratified_noalloc", "santa_status_string", "santa_last_error",
+           "santa_rope_init", "santa_rope_append", "santa_attend_workspace_size",
+           "santa_attend_chunk", "santa_decode_window")
 
 STREAM_READ_GROUPS = 4096  # SANTA_STREAM_READ_GROUPS: uint32 words of the sink
 STATIC_SCRATCH_BYTES = 64 << 20  # SANTA_STATIC_SCRATCH_BYTES
@@ -79,6 +85,33 @@ class santa_plan_info_t(ctypes.Structure):
                 ("kernels", ctypes.c_char_p)]
 
 
+class santa_chunk_t(ctypes.Structure):
+    _fields_ = [("q_start", ctypes.c_void_p), ("num_tokens", ctypes.c_int32),
+                ("max_tokens", ctypes.c_int32)]
+
+
+class santa_window_t(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
+class santa_rope_params_t(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("theta", ctypes.c_double), ("scaling", ctypes.c_int32), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("gain", ctypes.c_double)]
+
+
+class santa_rope_t(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("gain", ctypes.c_float), ("reserved", ctypes.c_int32), ("step", ctypes.c_uint64 * 64)]
+
+
+class santa_rows_t(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("positions", ctypes.c_void_p)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -110,6 +143,13 @@ def load() -> ctypes.CDLL:
     L.santa_set_options.argtypes = [OP]
     L.santa_get_options.argtypes = [OP]
     L.santa_plan_info.argtypes = [SP, KP, I32, I32, ctypes.POINTER(santa_plan_info_t)]
+    CP, WP, RP = (ctypes.POINTER(x) for x in (santa_chunk_t, santa_window_t, santa_rope_t))
+    L.santa_rope_init.argtypes = [ctypes.POINTER(santa_rope_params_t), RP]
+    L.santa_rope_append.argtypes = [ctypes.POINTER(santa_rows_t), KP, SP, CP, RP, P, P]
+    L.santa_attend_workspace_size.argtypes = [SP, KP, CP, WP]
+    L.santa_attend_workspace_size.restype = SZ
+    L.santa_attend_chunk.argtypes = [P, KP, SP, CP, WP, ctypes.c_float, P, P, SZ, P]
+    L.santa_decode_window.argtypes = [P, KP, SP, WP, ctypes.c_float, P, P, SZ, P]
     L.santa_status_string.argtypes = [ctypes.c_int]
     L.santa_status_string.restype = ctypes.c_char_p
     L.santa_last_error.restype = ctypes.c_char_p
@@ -117,7 +157,8 @@ def load() -> ctypes.CDLL:
                  "santa_decode_stratified", "santa_decode_bernoulli_qk", "santa_decode_flash",
                  "santa_decode_iid", "santa_stream_read", "santa_time_next_call",
                  "santa_set_options", "santa_get_options", "santa_plan_info",
-                 "santa_decode_stratified_noalloc"):
+                 "santa_decode_stratified_noalloc", "santa_rope_init", "santa_rope_append",
+                 "santa_attend_chunk", "santa_decode_window"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -203,6 +244,33 @@ def kt_feature_major(k_t: torch.Tensor) -> santa_kt_t:
     """k_t: [B, Hkv, d, n] with keys contiguous."""
     assert k_t.stride(-1) == 1
     return santa_kt_t(k_t.data_ptr(), k_t.stride(0), k_t.stride(1), k_t.stride(2))
+
+
+def chunk_of(q_start: Optional[torch.Tensor], num_tokens: int, max_tokens: int = 0) -> santa_chunk_t:
+    """New tokens of a batch: sequence b's are rows q_start[b] .. q_start[b + 1] - 1 (int32
+    [batch + 1] on the device; None: one token per sequence).  max_tokens: the most tokens a
+    sequence is expected to have (0: unknown)."""
+    if q_start is not None and (q_start.dtype != torch.int32 or not q_start.is_contiguous()):
+        raise TypeError("q_start must be a contiguous int32 tensor")
+    return santa_chunk_t(None if q_start is None else q_start.data_ptr(), int(num_tokens), int(max_tokens))
+
+
+def window_of(window: int, sinks: int = 0) -> santa_window_t:
+    """A sliding window of `window` keys (the token itself among them) and the first `sinks` keys."""
+    return santa_window_t(int(window), int(sinks))
+
+
+def rope_plan(rotary_dim: int = 128, interleaved: bool = False, theta: float = 10000.0,
+              scaling: str = "none", factor: float = 1.0, original_len: float = 0.0, low: float = 1.0,
+              high: float = 4.0, gain: float = 0.0) -> santa_rope_t:
+    """Rotary plan (santa_rope_init); scaling: "none", "linear", "base", "bands" or "ramp"."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+    p = santa_rope_params_t(int(rotary_dim), int(interleaved), float(theta), ROPE_SCALINGS[scaling],
+                            float(factor), float(original_len), float(low), float(high), float(gain))
+    plan = santa_rope_t()
+    _check(load().santa_rope_init(ctypes.byref(p), ctypes.byref(plan)))
+    return plan
 
 
 # ---------------------------------------------------------------------------
@@ -309,6 +377,104 @@ def santa_decode_flash(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, sc
                                      float(scale), int(tile), int(S_tile), _ptr(u), _ptr(idx_out),
                                      _ptr(out), _ptr(ws), ws.numel() * ws.element_size(),
                                      _stream(stream)))
+
+
+_TORCH_DTYPE = {SANTA_BF16: torch.bfloat16, SANTA_F32: torch.float32}
+
+
+def _rows_check(name: str, x: torch.Tensor, tokens: int, heads: int, dtype: torch.dtype,
+                contiguous: bool = True) -> None:
+    """x is [tokens, heads, 128] of dtype on the device, every token's heads in one run."""
+    if not x.is_cuda or x.dtype != dtype:
+        raise TypeError(f"{name} must be a {dtype} CUDA tensor")
+    if x.dim() != 3 or x.shape[0] != tokens or x.shape[1] != heads or x.shape[2] != 128:
+        raise ValueError(f"{name} must be [{tokens}, {heads}, 128], not {list(x.shape)}")
+    st = x.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != 128) or (contiguous and tokens > 1 and st[0] != heads * 128):
+        raise ValueError(f"{name}: every token's heads must be contiguous" + (", and the tokens" if contiguous else ""))
+
+
+def _launch(fn, device: torch.device, stream, *args) -> None:
+    """fn(*args, stream) with `device` current: its own current stream unless one is given."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(stream)))
+    else:
+        _check(fn(*args, _stream(stream)))
+
+
+def santa_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, kv: santa_kv_t,
+                      shape: santa_shape_t, chunk: Optional[santa_chunk_t], rope: Optional[santa_rope_t],
+                      q_out: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    """Rotate the new tokens' queries (into q_out) and keys, and store keys and values in the cache
+    of kv.  q [tokens, num_q_heads, 128], k and v [tokens, num_kv_heads, 128], possibly parts of one
+    projection's rows; q_out contiguous (q itself, if q is).  chunk None: one token per sequence."""
+    T = shape.batch if chunk is None else chunk.num_tokens
+    dt, Hkv = _TORCH_DTYPE[shape.dtype], shape.num_kv_heads
+    _rows_check("k", k, T, Hkv, dt, False)
+    _rows_check("v", v, T, Hkv, dt, False)
+    rows = santa_rows_t(None, k.data_ptr(), v.data_ptr(), 0, _row_stride(k), _row_stride(v), None)
+    if q is not None:
+        _rows_check("q", q, T, shape.num_q_heads, dt, False)
+        rows.q, rows.q_stride = q.data_ptr(), _row_stride(q)
+    if q_out is not None:
+        _rows_check("q_out", q_out, T, shape.num_q_heads, dt)
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.numel() < T or not positions.is_contiguous():
+            raise TypeError("positions must be a contiguous int32 tensor with a position per token")
+        rows.positions = positions.data_ptr()
+    _launch(load().santa_rope_append, k.device, stream, ctypes.byref(rows), ctypes.byref(kv),
+            ctypes.byref(shape), _ref(chunk), _ref(rope), _ptr(q_out))
+
+
+def _row_stride(x: torch.Tensor) -> int:
+    """Elements from one token to the next (one token: its heads' run, whatever torch says)."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * 128
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def santa_attend_workspace_size(shape: santa_shape_t, kv: santa_kv_t, chunk: Optional[santa_chunk_t] = None,
+                                window: Optional[santa_window_t] = None) -> int:
+    n = load().santa_attend_workspace_size(ctypes.byref(shape), ctypes.byref(kv), _ref(chunk), _ref(window))
+    if n == 0:
+        raise SantaError(SANTA_ERR_INVALID_ARG, "santa_attend_workspace_size: invalid arguments")
+    return int(n)
+
+
+def alloc_attend_workspace(shape: santa_shape_t, kv: santa_kv_t, chunk: Optional[santa_chunk_t] = None,
+                           window: Optional[santa_window_t] = None, device="cuda") -> torch.Tensor:
+    """alloc_workspace for santa_attend_chunk and santa_decode_window."""
+    n = santa_attend_workspace_size(shape, kv, chunk, window)
+    ws = torch.empty(n + 256, dtype=torch.uint8, device=device)
+    off = (-ws.data_ptr()) % 256
+    ws = ws[off:off + n]
+    santa_workspace_init(ws)
+    return ws
+
+
+def santa_attend_chunk(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, chunk: Optional[santa_chunk_t],
+                       window: Optional[santa_window_t], scale: float, out: torch.Tensor, ws: torch.Tensor,
+                       stream=None) -> None:
+    """Attention of the chunk's tokens over the cache that holds them; q, out [tokens, num_q_heads, 128]."""
+    T, dt = shape.batch if chunk is None else chunk.num_tokens, _TORCH_DTYPE[shape.dtype]
+    _rows_check("q", q, T, shape.num_q_heads, dt)
+    _rows_check("out", out, T, shape.num_q_heads, dt)
+    _launch(load().santa_attend_chunk, q.device, stream, q.data_ptr(), ctypes.byref(kv), ctypes.byref(shape),
+            _ref(chunk), _ref(window), scale, out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def santa_decode_window(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, window: santa_window_t,
+                        scale: float, out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """Decode step with a sliding window and sinks; q, out [batch, num_q_heads, 128]."""
+    dt = _TORCH_DTYPE[shape.dtype]
+    _rows_check("q", q, shape.batch, shape.num_q_heads, dt)
+    _rows_check("out", out, shape.batch, shape.num_q_heads, dt)
+    _launch(load().santa_decode_window, q.device, stream, q.data_ptr(), ctypes.byref(kv), ctypes.byref(shape),
+            _ref(window), scale, out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def santa_set_options(path: int = SANTA_PATH_AUTO, splits: int = 0) -> None:

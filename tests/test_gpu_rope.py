@@ -1,0 +1,305 @@
+"""santa_rope_append against float64: pair layouts, rotated parts, frequencies and far positions,
+cache layouts and element types, what is stored and what is left alone; and a prompt that goes
+through store, chunk attention and decode steps as a model would run them."""
+
+import math
+
+import pytest
+import torch
+
+from paper_2605_01910_amd import santa as S
+from tests.chunk_util import HALF, SCALE, Batch, attend, check
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+THETA = 500000.0
+RAGGED = [(1, 1), (0, 5), (3, 70), (33, 33), (1, 513), (17, 200), (0, 0)]
+
+
+def frequencies(R, device="cuda"):
+    i = torch.arange(R // 2, dtype=torch.float64, device=device)
+    return THETA ** (-2 * i / R)
+
+
+def rotated(x, pos, R, interleaved, freq=None, gain=1.0):
+    """float64 [T, H, 128] rotated at int64 positions [T]."""
+    x = x.double().clone()
+    a = pos.double()[:, None] * (frequencies(R) if freq is None else freq)
+    c, s = (a.cos() * gain)[:, None], (a.sin() * gain)[:, None]
+    i = torch.arange(R // 2, device=x.device)
+    p, r = (2 * i, 2 * i + 1) if interleaved else (i, i + R // 2)
+    u, v = x[..., p], x[..., r]
+    x[..., p], x[..., r] = u * c - v * s, v * c + u * s
+    return x
+
+
+def bound(x, dtype, R, angle=0.0):
+    """Rounding of the output (half a step of a value of at most |u| + |v|), and in 32 bits the
+    products, cos and sin: 8 half steps of 2^-24 of |u| + |v|, plus the angle's own error."""
+    pair = x.double().abs()
+    pair = pair.amax(-1, keepdim=True) * 2
+    return pair * (HALF[dtype] + 8 * 2.0 ** -24 + angle)
+
+
+def new_rows(bt, fused, seed=1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    H = bt.Hq + 2 * bt.Hkv
+    if fused:
+        rows = torch.randn(bt.T, H * 128, device="cuda", generator=g).to(bt.dtype)
+        return [p.unflatten(1, (-1, 128)) for p in rows.split([bt.Hq * 128, bt.Hkv * 128, bt.Hkv * 128], 1)]
+    return [torch.randn(bt.T, h, 128, device="cuda", generator=g).to(bt.dtype) for h in (bt.Hq, bt.Hkv, bt.Hkv)]
+
+
+def positions_of(bt):
+    """(sequence, cache position) of every token, -1 for rows behind the last sequence."""
+    seq = torch.full((bt.T,), -1, dtype=torch.int64, device="cuda")
+    pos = torch.zeros(bt.T, dtype=torch.int64, device="cuda")
+    for b, (c, L) in enumerate(bt.lens):
+        at = bt.starts[b]
+        seq[at:at + c] = b
+        pos[at:at + c] = torch.arange(L - c, L, device="cuda")
+    return seq, pos
+
+
+def e4m3(x):
+    """Codes nearest to float64 values, ties to even, saturated."""
+    return x.clamp(-448, 448).float().to(torch.float8_e4m3fn)
+
+
+CASES = {
+    "bf16": dict(),
+    "bf16_paged": dict(layout="paged", pad=3),
+    "bf16_hnd": dict(layout="hnd", gap=8),
+    "bf16_page_1": dict(layout="paged", page=1),
+    "f32": dict(dtype=F32, pad=1),
+    "f32_paged": dict(dtype=F32, layout="paged", Hq=3, Hkv=3),
+    "fp8": dict(fp8=True, gap=16),
+    "fp8_paged": dict(fp8=True, layout="paged", Hq=8, Hkv=1, pad=7),
+    "fp8_hnd": dict(fp8=True, layout="hnd", Hq=2, Hkv=2),
+    "many": dict(lens=[(i % 3, 3 + i) for i in range(200)], layout="paged"),
+    "long": dict(lens=[(1100, 1200), (3, 7)], pad=2),
+}
+
+
+@pytest.mark.parametrize("R,interleaved", [(128, False), (128, True), (64, False), (96, True), (16, False), (16, True)])
+@pytest.mark.parametrize("case", sorted(CASES))
+def test_rope_append(case, R, interleaved):
+    kw = dict(CASES[case])
+    bt = Batch(kw.pop("lens", RAGGED), seed=R, **kw)
+    q, k, v = new_rows(bt, fused=R != 64)
+    before = [x.clone() for x in (bt.k, bt.v)]
+    out = torch.full((bt.T, bt.Hq, 128), 7.0, dtype=bt.dtype, device="cuda")
+    plan = S.rope_plan(R, interleaved, THETA)
+    S.santa_rope_append(q, k, v, bt.kv(), bt.shape(), bt.chunk(), plan, out)
+    torch.cuda.synchronize()
+    seq, pos = positions_of(bt)
+    used = bt.starts[-1]
+    assert torch.all(out[used:] == 7.0)
+    want = rotated(q, pos, R, interleaved)
+    assert ((out.double() - want).abs() - bound(q, bt.dtype, R))[:used].amax() <= 0
+    assert torch.equal(out[:used, :, R:], q[:used, :, R:].to(bt.dtype))
+    kr = rotated(k, pos, R, interleaved)
+    for b, (c, L) in enumerate(bt.lens):
+        at, p = bt.starts[b], torch.arange(L - c, L, device="cuda")
+        gk, gv = bt.rows(bt.k, b, p), bt.rows(bt.v, b, p)
+        if bt.fp8:
+            for got, x, scale, exactly in ((gk, kr, bt.k_scale, False), (gv, v.double(), bt.v_scale, True)):
+                y = x[at:at + c] / scale[b].double()[:, None]
+                g = got.view(torch.float8_e4m3fn).double()
+                # half a step of e4m3 (2^-4 of the value, 2^-10 among subnormals), and the 32-bit error
+                # of the quotient where it decides a tie
+                slack = 0 if exactly else bound(k, F32, R)[at:at + c] / scale[b].double()[:, None]
+                lim = y.clamp(-448, 448)
+                assert ((g - lim).abs() <= lim.abs() * 2.0 ** -4 + 2.0 ** -10 + slack).all()
+            w = e4m3((v[at:at + c].float() / bt.v_scale[b][:, None]).double())
+            assert torch.equal(gv, w.view(torch.uint8))
+        else:
+            assert torch.equal(gv, v[at:at + c])
+            assert ((gk.double() - kr[at:at + c]).abs() <= bound(k, bt.dtype, R)[at:at + c]).all()
+    # nothing else of the cache changed
+    for cache, old in ((bt.k, before[0]), (bt.v, before[1])):
+        for b, (c, L) in enumerate(bt.lens):
+            p = torch.arange(L - c, L, device="cuda")
+            bt.put(cache, b, p, bt.rows(old, b, p))
+        assert torch.equal(torch.nan_to_num(cache.float(), 9), torch.nan_to_num(old.float(), 9))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_far_positions(interleaved):
+    """Explicit positions up to 2^31 - 1 and negative ones.  The reference's own angle, a double, is
+    off by 2^-53 of itself (2^31 radians: 2.4e-7); so is the plan's frequency."""
+    p = [0, 1, 2 ** 17 - 1, 10 ** 6 + 3, 2 ** 24 + 1, 2 ** 30, 2 ** 31 - 1, -1, -(2 ** 20)]
+    bt = Batch([(len(p), 20)], Hq=2, Hkv=1, dtype=F32, seed=2)
+    q, k, v = new_rows(bt, False)
+    out = torch.empty_like(q)
+    pos = torch.tensor(p, dtype=torch.int32, device="cuda")
+    S.santa_rope_append(q, k, v, bt.kv(), bt.shape(), bt.chunk(), S.rope_plan(128, interleaved, THETA), out, pos)
+    angle = pos.double().abs()[:, None, None] * 2.0 ** -51
+    assert ((out.double() - rotated(q, pos.long(), 128, interleaved)).abs() <= bound(q, F32, 128, angle)).all()
+    got = bt.rows(bt.k, 0, torch.arange(20 - len(p), 20, device="cuda")).double()
+    assert ((got - rotated(k, pos.long(), 128, interleaved)).abs() <= bound(k, F32, 128, angle)).all()
+
+
+@pytest.mark.parametrize("scaling", ["linear", "base", "bands", "ramp"])
+def test_scaled_frequencies(scaling):
+    """The plan's own steps (checked on the host against the formulas) as the angles."""
+    plan = S.rope_plan(128, False, THETA, scaling, 8.0, 8192, 1.0, 32.0)
+    freq = torch.tensor([s / 2.0 ** 64 * 2 * math.pi for s in plan.step], dtype=torch.float64, device="cuda")
+    bt = Batch([(50, 40000)], Hq=4, Hkv=1, dtype=F32, seed=3)
+    q, k, v = new_rows(bt, False)
+    out = torch.empty_like(q)
+    S.santa_rope_append(q, k, v, bt.kv(), bt.shape(), bt.chunk(), plan, out)
+    _, pos = positions_of(bt)
+    want = rotated(q, pos, 128, False, freq, plan.gain)
+    assert ((out.double() - want).abs() <= bound(q, F32, 128) * 1.25).all()  # (the gain: at most 1.21)
+
+
+def test_rotation_undone_by_negative_positions():
+    """The rotation's transpose is the rotation at -position: its gradient is the same call."""
+    bt = Batch([(64, 500)], Hq=4, Hkv=2, dtype=F32, seed=4)
+    q, k, v = new_rows(bt, False)
+    out, back = torch.empty_like(q), torch.empty_like(q)
+    pos = torch.arange(436, 500, dtype=torch.int32, device="cuda")
+    plan = S.rope_plan(128, False, THETA)
+    S.santa_rope_append(q, k, v, bt.kv(), bt.shape(), bt.chunk(), plan, out)
+    S.santa_rope_append(out, k, v, bt.kv(), bt.shape(), bt.chunk(), plan, back, -pos)
+    assert ((back.double() - q.double()).abs() <= 3 * bound(q, F32, 128)).all()
+
+
+def test_in_place_without_queries_and_without_rotation():
+    bt = Batch(RAGGED, seed=5, layout="paged", pad=2)
+    q, k, v = new_rows(bt, False)
+    plan, used = S.rope_plan(64, True, THETA), bt.starts[-1]
+    want = torch.zeros_like(q)
+    S.santa_rope_append(q, k, v, bt.kv(), bt.shape(), bt.chunk(), plan, want)
+    k1, v1 = bt.k.clone(), bt.v.clone()
+    same = q.clone()
+    S.santa_rope_append(same, k, v, bt.kv(), bt.shape(), bt.chunk(), plan, same)
+    assert torch.equal(same[:used], want[:used]) and torch.equal(same[used:], q[used:])
+    bt.k.zero_(), bt.v.zero_()
+    S.santa_rope_append(None, k, v, bt.kv(), bt.shape(), bt.chunk(), plan, None)
+    for b, (c, L) in enumerate(bt.lens):
+        p = torch.arange(L - c, L, device="cuda")
+        assert torch.equal(bt.rows(bt.k, b, p), bt.rows(k1, b, p)) and torch.equal(bt.rows(bt.v, b, p), bt.rows(v1, b, p))
+    S.santa_rope_append(None, k, v, bt.kv(), bt.shape(), bt.chunk(), None, None)
+    for b, (c, L) in enumerate(bt.lens):
+        p, at = torch.arange(L - c, L, device="cuda"), bt.starts[b]
+        assert torch.equal(bt.rows(bt.k, b, p), k[at:at + c])
+
+
+def test_fp8_codes():
+    """Ties to even, saturation and NaN; every finite code is reached from its own value."""
+    bt = Batch([(1, 1), (1, 1)], Hq=1, Hkv=1, fp8=True, seed=6)
+    bt.v_scale.fill_(0.5), bt.k_scale.fill_(0.25)
+    codes = torch.arange(256, dtype=torch.int32, device="cuda").to(torch.uint8)
+    x = codes.view(torch.float8_e4m3fn).float().reshape(2, 1, 128)
+    q, k, v = new_rows(bt, False)
+    v.copy_(x * 0.5)
+    special = [1.0625, 1.1875, -1.0625, 2.0 ** -10, 3 * 2.0 ** -10, 448.0, 463.0, 1e6, -1e6, math.inf, -math.inf, math.nan]
+    k.zero_()
+    k[0, 0, :len(special)] = torch.tensor(special, device="cuda").to(BF) * 0.25
+    S.santa_rope_append(None, k, v, bt.kv(), bt.shape(), bt.chunk(), None, None)
+    got = bt.v.view(torch.float8_e4m3fn).float().reshape(2, 1, 128)
+    assert torch.equal(torch.nan_to_num(got, 999), torch.nan_to_num(x, 999))
+    got = bt.k[0, 0, 0, :len(special)].view(torch.float8_e4m3fn).float().tolist()
+    assert got[:11] == [1.0, 1.25, -1.0, 0.0, 2.0 ** -8, 448.0, 448.0, 448.0, -448.0, 448.0, -448.0]
+    assert math.isnan(got[11])
+
+
+def test_tokens_without_a_row_are_not_stored():
+    """Tokens before position 0 and tokens whose page is negative."""
+    bt = Batch([(5, 20), (3, 40)], layout="paged", seed=7)
+    q, k, v = new_rows(bt, False)
+    bt.ctx[0] = 3
+    bt.table[1, 2] = -1  # positions 37 .. 39 of sequence 1
+    before = bt.k.clone()
+    out = torch.zeros_like(q)
+    plan = S.rope_plan(128, False, THETA)
+    S.santa_rope_append(q, k, v, bt.kv(), bt.shape(), bt.chunk(), plan, out)
+    pos = torch.tensor([-2, -1, 0, 1, 2, 37, 38, 39], device="cuda")
+    assert ((out.double() - rotated(q, pos, 128, False)).abs() <= bound(q, BF, 128)).all()
+    changed = (torch.nan_to_num(bt.k, 9) != torch.nan_to_num(before, 9)).any(-1).any(1).nonzero().tolist()
+    page = bt.table[0, 0].item()
+    assert sorted(changed) == [[page, 0], [page, 1], [page, 2]]
+
+
+def test_offsets_past_32_bits():
+    bt = Batch([(20, 300), (1, 900)], Hq=8, Hkv=8, layout="paged", pages=135000, seed=8)
+    assert bt.k.shape[0] * bt.k.stride(0) > 2 ** 31 and bt.table.min() > 130000
+    q, k, v = new_rows(bt, True)
+    out = torch.zeros(bt.T, bt.Hq, 128, dtype=BF, device="cuda")
+    S.santa_rope_append(q, k, v, bt.kv(), bt.shape(), bt.chunk(), S.rope_plan(128, False, THETA), out)
+    for b, (c, L) in enumerate(bt.lens):
+        at = bt.starts[b]
+        assert torch.equal(bt.rows(bt.v, b, torch.arange(L - c, L, device="cuda")), v[at:at + c])
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(layout="paged"), dict(dtype=F32, layout="hnd"), dict(fp8=True, layout="paged")],
+                         ids=["bf16", "paged", "f32", "fp8"])
+@pytest.mark.parametrize("window", [None, (50, 4)], ids=str)
+def test_prompt_in_pieces_then_decode(kw, window):
+    """Two prompts through store and attention in pieces (one of them beside the other's single
+    tokens), then decode steps, the store captured with the attention in a graph.  Every step's
+    output is checked on the cache as the calls left it."""
+    lens, Hq, Hkv = (150, 97), 8, 2
+    bt = Batch([(L, L) for L in lens], Hq=Hq, Hkv=Hkv, seed=21, n=160, **kw)
+    plan = S.rope_plan(128, False, THETA)
+    done = [0, 0]
+    for step in ((70, 1), (0, 60), (80, 1), (0, 35)):
+        part = Batch([(c, done[b] + c) for b, c in enumerate(step)], Hq=Hq, Hkv=Hkv, seed=sum(step), n=160, **kw)
+        part.k, part.v, part.k_scale, part.v_scale = bt.k, bt.v, bt.k_scale, bt.v_scale
+        if bt.layout == "paged":
+            part.table = bt.table
+        q, k, v = new_rows(part, True, seed=step[0] + step[1])
+        S.santa_rope_append(q, k, v, part.kv(), part.shape(), part.chunk(), plan, part.q)
+        _, pos = positions_of(part)
+        assert ((part.q.double() - rotated(q, pos, 128, False)).abs() <= bound(q, part.dtype, 128)).all()
+        check(part, attend(part, window), window)
+        done = [d + c for d, c in zip(done, step)]
+    assert tuple(done) == lens
+    # decode: one graph holds the step of both sequences; ctx_len moves on between replays
+    dec = Batch([(1, L + 1) for L in lens], Hq=Hq, Hkv=Hkv, seed=30, n=160, **kw)
+    dec.k, dec.v, dec.k_scale, dec.v_scale = bt.k, bt.v, bt.k_scale, bt.v_scale
+    if bt.layout == "paged":
+        dec.table = bt.table
+    q, k, v = new_rows(dec, True, seed=31)
+    kv, sh = dec.kv(), dec.shape()
+    win = S.window_of(*window) if window else None
+    ws, out = S.alloc_attend_workspace(sh, kv, None, win), torch.full_like(dec.q, 7.0)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        S.santa_rope_append(q, k, v, kv, sh, None, plan, dec.q)
+        if window:
+            S.santa_decode_window(dec.q, kv, sh, win, SCALE, out, ws)
+        else:
+            S.santa_attend_chunk(dec.q, kv, sh, None, None, SCALE, out, ws)
+    for i in range(4):
+        dec.lens = [(1, L + 1 + i) for L in lens]
+        dec.ctx.copy_(torch.tensor([L for _, L in dec.lens], dtype=torch.int32))
+        q.copy_(torch.randn(q.shape, device="cuda"))
+        k.copy_(torch.randn(k.shape, device="cuda"))
+        v.copy_(torch.randn(v.shape, device="cuda"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        check(dec, out, window)
+        if not window and not dec.fp8:  # the library's own dense step agrees within both bounds
+            dense = torch.full_like(out, 7.0)
+            wd = S.alloc_workspace(sh, kv, 1, S.SANTA_KIND_DENSE)
+            S.santa_decode_dense(dec.q, kv, sh, SCALE, dense, wd)
+            check(dec, dense)
+
+
+def test_argument_checks():
+    bt = Batch([(2, 40)], seed=22)
+    q, k, v = new_rows(bt, False)
+    kv, sh, ch, plan, out = bt.kv(), bt.shape(), bt.chunk(), S.rope_plan(), torch.empty_like(q)
+    bad = [dict(q=q.float()), dict(k=k[:1]), dict(v=v[:, :1]), dict(q_out=out.transpose(0, 1)), dict(k=k.cpu()),
+           dict(q_out=None), dict(positions=torch.zeros(1, dtype=torch.int32, device="cuda")),
+           dict(positions=torch.zeros(2, device="cuda")), dict(k=k[..., ::2].repeat(1, 1, 2)[..., ::2]), dict(rope=None)]
+    for kw in bad:
+        args = dict(q=q, k=k, v=v, kv=kv, shape=sh, chunk=ch, rope=plan, q_out=out)
+        args.update(kw)
+        with pytest.raises((S.SantaError, ValueError, TypeError)):
+            S.santa_rope_append(**args)
