@@ -300,10 +300,10 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
   const int64_t n = std::min(p.B, ch.num_tokens);
   p.tiles = (ch.num_tokens - n) / p.tile_tokens + n;
   const int64_t keys = win ? std::min<int64_t>(kv->n_k, (int64_t)win->sinks + win->window + p.tile_tokens - 1) : kv->n_k;
-  p.step = p.few ? 128 : p.elem == 1 ? 32 : 64;
+  p.step = p.few || p.elem == 1 ? 32 : 64;
   // about two workgroups per CU, none with fewer keys than its start costs
   const int64_t groups = p.tiles * p.Hkv;
-  int64_t T = std::min<int64_t>(512 / groups, keys / (p.few ? 128 : 256));
+  int64_t T = std::min<int64_t>(512 / groups, p.few ? (keys + 127) / 128 : keys / 256);
   if (g_opts.splits > 0) T = g_opts.splits;
   p.T = (int)std::max<int64_t>(1, std::min<int64_t>(T, santa::kMaxSplits));
   size_t off = 0;

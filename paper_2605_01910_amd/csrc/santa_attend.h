@@ -64,16 +64,18 @@ __device__ __forceinline__ RowSight row_sight(const KeyMap &km, int p, int windo
   return s;
 }
 
-// 16-byte chunk c of LDS row `row` stands at chunk c ^ swizzle: the lanes of a
-// key read take one chunk of 32 rows, those of a value read four rows' (or,
-// 32-bit, two rows') same chunks; either way they spread over all banks.
+// Rows in LDS.  L: bfloat16, float32, or FP8 codes as they are in the cache
+// (the operands are widened as they are read).  16-byte chunk c of row `row`
+// stands at chunk c ^ swizzle: the lanes of a key read take one chunk of 32
+// rows, those of a value read the same chunks of four rows (codes: of 16, 32-bit
+// values: of two); either way they spread over all banks.
 template <typename L>
 __device__ __forceinline__ int k_swz(int row) {
-  return row & 15;
+  return sizeof(L) == 1 ? (row >> 1) & 7 : row & 15;
 }
 template <typename L>
 __device__ __forceinline__ int v_swz(int row) {
-  return sizeof(L) == 2 ? (row & 3) << 2 : ((row >> 2) & 1) << 3;
+  return sizeof(L) == 1 ? (row >> 1) & 7 : sizeof(L) == 2 ? (row & 3) << 2 : ((row >> 2) & 1) << 3;
 }
 template <typename L>
 constexpr int lds_row() {
@@ -115,7 +117,19 @@ __device__ __forceinline__ void load_rows(AQ<float> &q, const float *p, bool val
 }
 
 // Scores of keys [32 t, 32 t + 32) of the tile at K, raw (before the scale).
-__device__ __forceinline__ af32x16 score_block(const AQ<uint16_t> &q, const char *K, int t) {
+__device__ __forceinline__ af32x16 score_block(const AQ<uint16_t> &q, const char *K, int t, uint8_t) {
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  const char *row = K + (32 * t + r) * lds_row<uint8_t>() + 8 * h;
+  const int x = (r >> 1) & 7;
+  af32x16 s = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const Chunk<uint8_t> k{*reinterpret_cast<const uint2 *>(row + ((i ^ x) << 4))};
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, k.to_bf16()), q.f[i], s, 0, 0, 0);
+  }
+  return s;
+}
+__device__ __forceinline__ af32x16 score_block(const AQ<uint16_t> &q, const char *K, int t, uint16_t) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   const char *row = K + (32 * t + r) * lds_row<uint16_t>();
   const int x = h ^ (r & 15);
@@ -127,7 +141,7 @@ __device__ __forceinline__ af32x16 score_block(const AQ<uint16_t> &q, const char
   }
   return s;
 }
-__device__ __forceinline__ af32x16 score_block(const AQ<float> &q, const char *K, int t) {
+__device__ __forceinline__ af32x16 score_block(const AQ<float> &q, const char *K, int t, float) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   const char *row = K + (32 * t + r) * lds_row<float>();
   const int x = h ^ (r & 15);
@@ -151,14 +165,29 @@ struct RowState {
   af32x16 o[4];
 };
 
-// Four keys' values as one operand half: features 32 n + l % 32 of keys
-// row .. row + 3 (row: a multiple of 4 that depends on l / 32).
+// Values as the left operand of O^T += V^T P^T: features 32 n + l % 32 of the
+// keys row .. row + 3 and row + 8 .. row + 11 (row: 16 b + 4 (l / 32)), the
+// ones whose weights the lane holds.
 __device__ __forceinline__ as16x4 value_quad(const char *V, int row, int n) {
   const int l = threadIdx.x & 15, g = (threadIdx.x >> 4) & 1, k = l >> 2;
   const char *p = V + (row + k) * lds_row<uint16_t>() + (((4 * n + 2 * g + ((l & 3) >> 1)) ^ (k << 2)) << 4) +
                   (l & 1) * 8;
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
       (__attribute__((address_space(3))) as16x4 *)(reinterpret_cast<const as16x4 *>(p)));
+}
+__device__ __forceinline__ uint4 value_operand(const char *V, int row, int n, uint16_t) {
+  const uint2 u = __builtin_bit_cast(uint2, value_quad(V, row, n));
+  const uint2 v = __builtin_bit_cast(uint2, value_quad(V, row + 8, n));
+  return make_uint4(u.x, u.y, v.x, v.y);
+}
+__device__ __forceinline__ uint4 value_operand(const char *V, int row, int n, uint8_t) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  const int l = threadIdx.x & 15, g = (threadIdx.x >> 4) & 1, k = l >> 1;  // the lane's eighth of 8 rows x 16 codes
+  const int rr = row + (k & 3) + 2 * (k & 4);
+  const char *p = V + rr * lds_row<uint8_t>() + (((2 * n + g) ^ v_swz<uint8_t>(rr)) << 4) + (l & 1) * 8;
+  const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+      (__attribute__((address_space(3))) i32x2 *)(reinterpret_cast<const i32x2 *>(p)));
+  return Chunk<uint8_t>{make_uint2((unsigned)w[0], (unsigned)w[1])}.to_bf16();
 }
 
 // Non-finite values stand apart: a key that some rows of the tile do not see
@@ -183,10 +212,10 @@ __device__ __forceinline__ float mark_value(int kind) {
   return kind == 0 ? kInf : kind == 1 ? -kInf : __builtin_nanf("");
 }
 
-// O^T += V^T P^T over keys [32 t, 32 t + 32) of the tile at V.  EDGE: some row
-// may not see some of the keys (their weights are 0).
-template <bool EDGE>
-__device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, uint16_t) {
+// O^T += V^T P^T over keys [32 t, 32 t + 32) of the tile at V (rows of type L).
+// EDGE: some row may not see some of the keys (their weights are 0).
+template <bool EDGE, typename L, std::enable_if_t<sizeof(L) <= 2, int> = 0>
+__device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, L) {
   const int h = (threadIdx.x >> 5) & 1;
   abf16x8 pf[2];
 #pragma unroll
@@ -199,10 +228,7 @@ __device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const
     uint32_t bad = 0;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const int row = 32 * t + 16 * b + 4 * h;
-      const as16x4 x = value_quad(V, row, n), y = value_quad(V, row + 8, n);
-      const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
-      w[b] = make_uint4(u.x, u.y, v.x, v.y);
+      w[b] = value_operand(V, 32 * t + 16 * b + 4 * h, n, L{});
       if constexpr (EDGE)
         bad |= nonfinite2(w[b].x) | nonfinite2(w[b].y) | nonfinite2(w[b].z) | nonfinite2(w[b].w);
     }
@@ -229,8 +255,8 @@ __device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const
       st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, w[b]), pf[b], st.o[n], 0, 0, 0);
   }
 }
-template <bool EDGE>
-__device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, float) {
+template <bool EDGE, typename L, std::enable_if_t<sizeof(L) == 4, int> = 0>
+__device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, L) {
   const int lane = threadIdx.x & 63, d = lane & 31, h = lane >> 5;
 #pragma unroll
   for (int n = 0; n < 4; ++n) {
@@ -260,17 +286,14 @@ __device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const
   }
 }
 
-// One step of the online softmax over NB blocks of 32 keys whose K and V rows
-// are in LDS; v0: the first key's number.
-template <typename L, int NB, bool EDGE>
-__device__ __forceinline__ void attend_step(RowState &st, const AQ<L> &q, const char *K, const char *V, int v0,
-                                            const RowSight &rs, float c) {
+// One step of the online softmax: raw scores of NB blocks of 32 keys from
+// number v0 on become weights, and the running state follows.
+template <int NB, bool EDGE>
+__device__ __forceinline__ void softmax_step(RowState &st, af32x16 (&s)[NB], int v0, const RowSight &rs, float c) {
   const int h = (threadIdx.x >> 5) & 1;
-  af32x16 s[NB];
   float tm = -kInf;
 #pragma unroll
-  for (int t = 0; t < NB; ++t) {
-    s[t] = score_block(q, K, t);
+  for (int t = 0; t < NB; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if constexpr (EDGE) {
@@ -279,7 +302,6 @@ __device__ __forceinline__ void attend_step(RowState &st, const AQ<L> &q, const 
       }
       tm = fmaxf(tm, s[t][i]);
     }
-  }
   tm = xor32_max(tm);
   const float mn = fmaxf(st.m, tm);
   const float mc = mn == -kInf ? 0.0f : mn * c;  // nothing visible yet: every weight is 0
@@ -293,54 +315,117 @@ __device__ __forceinline__ void attend_step(RowState &st, const AQ<L> &q, const 
     st.m = mn;
   }
 #pragma unroll
-  for (int t = 0; t < NB; ++t) {
+  for (int t = 0; t < NB; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       s[t][i] = fast_exp2(fmaf(s[t][i], c, -mc));
       st.l += s[t][i];
     }
-    add_values<EDGE>(st, s[t], V, t, L{});
-  }
 }
 
 // ---------------------------------------------------------------------------
 // Cache rows into LDS
 // ---------------------------------------------------------------------------
-// KEYS rows of K and V, keys v0 .. of the tile, by a team of TEAM lanes (`tl`:
-// this lane's number); rows past `end` are zeros.
-template <typename E, bool PAGED, int KEYS, int TEAM>
-__device__ __forceinline__ void stage_rows(const KvView &kv, int b, int kvh, const KeyMap &km, int v0, int end,
-                                           int tl, char *K, char *V) {
-  using L = LE<E>;
-  constexpr int CPR = kHeadDim * (int)sizeof(E) / 16;  // 16-byte chunks of a cache row
-  constexpr int N = KEYS * CPR / TEAM;
-  static_assert(KEYS * CPR % TEAM == 0, "whole chunks per lane");
-  const char *kb = static_cast<const char *>(kv.k), *vb = static_cast<const char *>(kv.v);
+// A wave's share of a tile, R consecutive rows: NL copies of 1 KiB, RPL rows
+// each, straight into LDS (no registers in between).  Copy n's lane takes chunk
+// `lane % CPR` of its row as the swizzle moves it, from row n * RPL + lane / CPR.
+template <typename E, bool PAGED, int R>
+struct RowCopies {
+  static constexpr int CPR = kHeadDim * (int)sizeof(E) / 16, RPL = 64 / CPR, NL = R / RPL;
+  static_assert(R % RPL == 0, "whole copies");
+  const KvView &kv;
+  const KeyMap km;
+  int64_t base;    // elements to the sequence's (contiguous) or the pool's (paged) KV head
+  int b, end;      // rows at or past `end` repeat the last one before it
+  int win, first, upto;  // paged: lane i holds the sequence's table entry first + i, up to `upto`
+  int64_t at[NL];  // byte offsets of the rows of the tile that is copied next
+
+  __device__ __forceinline__ RowCopies(const KvView &kv_, const KeyMap &km_, int b_, int kvh, int end_)
+      : kv(kv_), km(km_), b(b_), end(end_), win(0), first(0), upto(-1) {
+    base = (int64_t)kvh * kv.sh + (PAGED ? 0 : (int64_t)b * kv.sb);
+  }
+  __device__ __forceinline__ static int row_of(int n) { return n * RPL + (threadIdx.x & 63) / CPR; }
+
+  // The rows from key v0 on (v0 < end) are next.
+  __device__ __forceinline__ void seek(int v0) {
+    if constexpr (PAGED) {
+      const int last = min(v0 + R, end) - 1;
+      const int e0 = km.pos(v0) >> kv.ps_log2, e1 = km.pos(last) >> kv.ps_log2;
+      const bool gap = v0 < km.n0 && last >= km.n0;  // sinks and window in one tile: entries far apart
+      if (!gap && (e0 < first || e1 > upto)) {
+        first = e0;
+        upto = min(e0 + 63, km.pos((v0 < km.n0 ? min(km.n0, end) : end) - 1) >> kv.ps_log2);  // the run's last key
+        win = kv.bt[(int64_t)b * kv.max_pages + min(e0 + (int)(threadIdx.x & 63), upto)];
+      }
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int i = n * TEAM + tl, row = i / CPR, ch = i % CPR, v = v0 + row;
-    uint4 kw = make_uint4(0, 0, 0, 0), vw = make_uint4(0, 0, 0, 0);
-    if (v < end) {
-      const int64_t off = row_offset<PAGED>(kv, b, kvh, km.pos(v)) * (int64_t)sizeof(E) + ch * 16;
-      kw = *reinterpret_cast<const uint4 *>(kb + off);
-      vw = *reinterpret_cast<const uint4 *>(vb + off);
-    }
-    char *kd = K + row * lds_row<L>(), *vd = V + row * lds_row<L>();
-    const int kx = k_swz<L>(row), vx = v_swz<L>(row);
-    if constexpr (sizeof(E) == 1) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const Chunk<uint8_t> a{half ? make_uint2(kw.z, kw.w) : make_uint2(kw.x, kw.y)};
-        const Chunk<uint8_t> c{half ? make_uint2(vw.z, vw.w) : make_uint2(vw.x, vw.y)};
-        *reinterpret_cast<uint4 *>(kd + (((2 * ch + half) ^ kx) << 4)) = a.to_bf16();
-        *reinterpret_cast<uint4 *>(vd + (((2 * ch + half) ^ vx) << 4)) = c.to_bf16();
+      for (int n = 0; n < NL; ++n) {
+        const int pos = km.pos(min(v0 + row_of(n), end - 1)), e = pos >> kv.ps_log2;
+        const int page = gap ? kv.bt[(int64_t)b * kv.max_pages + e] : __shfl(win, e - first);
+        at[n] = (base + (int64_t)page * kv.sb + (int64_t)(pos & ((1 << kv.ps_log2) - 1)) * kv.sn) * (int64_t)sizeof(E);
       }
     } else {
-      *reinterpret_cast<uint4 *>(kd + ((ch ^ kx) << 4)) = kw;
-      *reinterpret_cast<uint4 *>(vd + ((ch ^ vx) << 4)) = vw;
+#pragma unroll
+      for (int n = 0; n < NL; ++n)
+        at[n] = (base + (int64_t)km.pos(min(v0 + row_of(n), end - 1)) * kv.sn) * (int64_t)sizeof(E);
     }
   }
+
+  // Start copying the rows of `src` (kv.k or kv.v) to LDS rows row0 .. of `dst`.
+  // NT: read once by the whole call, so that they do not displace other lines.
+  template <bool VALUES, bool NT>
+  __device__ __forceinline__ void copy(const void *src, char *dst, int row0) const {
+    const unsigned m = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_addr(dst + row0 * lds_row<E>()));
+    const int p = (threadIdx.x & 63) % CPR;
+#pragma unroll
+    for (int n = 0; n < NL; ++n) {
+      const int row = row0 + row_of(n), ch = p ^ (VALUES ? v_swz<E>(row) : k_swz<E>(row));
+      const char *g = static_cast<const char *>(src) + at[n] + ch * 16;
+      if constexpr (NT)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
+                     ::"s"(m + n * 1024u), "v"(g) : "memory", "m0");
+      else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                     ::"s"(m + n * 1024u), "v"(g) : "memory", "m0");
+    }
+  }
+};
+
+// At most N of the wave's copies (and loads) outstanding.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// Every LDS read of the wave has returned: what it read may be overwritten.
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// FP8 rows of a full tile: codes through registers, widened on the way into LDS,
+// once for the four waves.  NC: 16-byte chunks of K and of V per lane.
+template <bool PAGED, int KEYS>
+struct WidenedRows {
+  static constexpr int NC = KEYS * 8 / kThreads;
+  uint4 k[NC], v[NC];
+  __device__ __forceinline__ void load(const KvView &kv, const KeyMap &km, int b, int kvh, int v0, int end) {
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const int i = n * kThreads + threadIdx.x;
+      const int64_t off = row_offset<PAGED>(kv, b, kvh, km.pos(min(v0 + i / 8, end - 1))) + (i % 8) * 16;
+      k[n] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(kv.k) + off);
+      v[n] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(kv.v) + off);
+    }
+  }
+  __device__ __forceinline__ void store(char *K, char *V) const {
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const int i = n * kThreads + threadIdx.x, row = i / 8, c = 2 * (i % 8);
+      char *kd = K + row * lds_row<uint16_t>(), *vd = V + row * lds_row<uint16_t>();
+      const int kx = k_swz<uint16_t>(row), vx = v_swz<uint16_t>(row);
+      *reinterpret_cast<uint4 *>(kd + ((c ^ kx) << 4)) = Chunk<uint8_t>{make_uint2(k[n].x, k[n].y)}.to_bf16();
+      *reinterpret_cast<uint4 *>(kd + (((c + 1) ^ kx) << 4)) = Chunk<uint8_t>{make_uint2(k[n].z, k[n].w)}.to_bf16();
+      *reinterpret_cast<uint4 *>(vd + ((c ^ vx) << 4)) = Chunk<uint8_t>{make_uint2(v[n].x, v[n].y)}.to_bf16();
+      *reinterpret_cast<uint4 *>(vd + (((c + 1) ^ vx) << 4)) = Chunk<uint8_t>{make_uint2(v[n].z, v[n].w)}.to_bf16();
+    }
+  }
+};
 
 // ---------------------------------------------------------------------------
 // Tiles
@@ -416,7 +501,8 @@ __device__ __forceinline__ Scale score_scale(const AttendArgs &a, float2 sc) {
 }
 
 // Many rows: 128 rows, 32 per wave; K and V tiles of KEYS keys shared by the
-// four waves.
+// four waves, two of each in LDS: the next keys are copied while this tile's
+// scores are taken, the next values while its weights are used.
 template <typename E>
 constexpr int many_keys() {
   return sizeof(E) == 4 ? 32 : 64;
@@ -424,9 +510,9 @@ constexpr int many_keys() {
 template <typename E, bool PAGED>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttendArgs a) {
   using L = LE<E>;
-  constexpr int KEYS = many_keys<E>(), NB = KEYS / 32;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  char *K = lds, *V = lds + KEYS * lds_row<L>();
+  constexpr int KEYS = many_keys<E>(), NB = KEYS / 32, TB = KEYS * lds_row<L>();
+  constexpr bool WIDEN = sizeof(E) == 1;
+  extern __shared__ __attribute__((aligned(16))) char lds[];  // K0, K1, V0, V1 (FP8: K0, V0)
   const Work w = find_work(a, kManyRows);
   if (!w.any) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -439,23 +525,78 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   // what all of the wave's rows see, and what any of them does
   const bool live = 32 * wave < w.rows;
   const Row first = tile_row(a, w, 32 * wave), last = tile_row(a, w, min(32 * wave + 31, w.rows - 1));
+  RowSight see = row.see;
+  see.hi = min(see.hi, w.v_end);
+  const int all_hi = min(first.see.hi, w.v_end);
 
   RowState st;
   st.m = -kInf;
   st.l = 0.0f;
 #pragma unroll
   for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
-  for (int v0 = w.v_begin; v0 < w.v_end; v0 += KEYS) {
-    const int v1 = min(v0 + KEYS, w.v_end);
-    __syncthreads();
-    stage_rows<E, PAGED, KEYS, kThreads>(a.kv, w.at.b, w.kvh, w.km, v0, w.v_end, tid, K, V);
-    __syncthreads();
-    if (!live || v0 >= last.see.hi || (v1 <= first.see.lo && v0 >= first.see.sv)) continue;
-    const bool whole = v0 + KEYS <= min(first.see.hi, w.v_end) && (v0 >= last.see.lo || v0 + KEYS <= last.see.sv);
-    RowSight see = row.see;
-    see.hi = min(see.hi, w.v_end);
-    if (whole) attend_step<L, NB, false>(st, q, K, V, v0, see, scale.c);
-    else attend_step<L, NB, true>(st, q, K, V, v0, see, scale.c);
+  // (the wave has no share in a tile that none of its rows see)
+  auto step = [&](int v0, const char *K, const char *V, auto between) {
+    const bool mine = live && v0 < last.see.hi && (v0 + KEYS > first.see.lo || v0 < first.see.sv);
+    const bool whole = v0 + KEYS <= all_hi && (v0 >= last.see.lo || v0 + KEYS <= last.see.sv);
+    af32x16 s[NB];
+    if (mine) {
+#pragma unroll
+      for (int t = 0; t < NB; ++t) s[t] = score_block(q, K, t, L{});
+      if (whole) softmax_step<NB, false>(st, s, v0, see, scale.c);
+      else softmax_step<NB, true>(st, s, v0, see, scale.c);
+    }
+    between();
+    if (mine) {
+      if (whole) {
+#pragma unroll
+        for (int t = 0; t < NB; ++t) add_values<false>(st, s[t], V, t, L{});
+      } else {
+#pragma unroll
+        for (int t = 0; t < NB; ++t) add_values<true>(st, s[t], V, t, L{});
+      }
+    }
+  };
+  if constexpr (WIDEN) {
+    WidenedRows<PAGED, KEYS> next;
+    char *K = lds, *V = lds + TB;
+    if (w.v_begin < w.v_end) next.load(a.kv, w.km, w.at.b, w.kvh, w.v_begin, w.v_end);
+    for (int v0 = w.v_begin; v0 < w.v_end; v0 += KEYS) {
+      __syncthreads();
+      next.store(K, V);
+      __syncthreads();
+      if (v0 + KEYS < w.v_end) next.load(a.kv, w.km, w.at.b, w.kvh, v0 + KEYS, w.v_end);
+      step(v0, K, V, [] {});
+    }
+  } else {
+    constexpr int R = KEYS / 4;
+    RowCopies<E, PAGED, R> rc(a.kv, w.km, w.at.b, w.kvh, w.v_end);
+    const int r0 = R * wave;
+    auto begin = [&](int v0) { rc.seek(min(v0 + r0, w.v_end - 1)); };
+    if (w.v_begin < w.v_end) {
+      begin(w.v_begin);
+      rc.template copy<false, false>(a.kv.k, lds, r0);
+      rc.template copy<true, false>(a.kv.v, lds + 2 * TB, r0);
+    }
+    int turn = 0;
+    for (int v0 = w.v_begin; v0 < w.v_end; v0 += KEYS) {
+      const bool more = v0 + KEYS < w.v_end;
+      char *K = lds + turn * TB, *V = lds + (2 + turn) * TB;
+      // this tile's keys are here when every wave's copies are; all waves are
+      // done with the other key tile since the barrier before their values
+      wait_copies<decltype(rc)::NL>();
+      __syncthreads();
+      if (more) {
+        begin(v0 + KEYS);
+        rc.template copy<false, false>(a.kv.k, lds + (turn ^ 1) * TB, r0);
+      }
+      step(v0, K, V, [&] {
+        if (more) wait_copies<decltype(rc)::NL>();
+        else wait_copies<0>();
+        __syncthreads();
+        if (more) rc.template copy<true, false>(a.kv.v, lds + (2 + (turn ^ 1)) * TB, r0);
+      });
+      turn ^= 1;
+    }
   }
 
   const float l = xor32_sum(st.l);
@@ -482,10 +623,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 }
 
-// Few rows: up to 32, the same for all four waves, which take 32 keys in turn
-// and join their results through LDS at the end.
+// Few rows: up to 32, the same for all four waves, which share out the keys:
+// each wave streams its own run of them through its own two slots of LDS, the
+// keys' and the values' in turn, with no barrier inside the stream, and keeps
+// its own softmax; they join their results through LDS at the end.
+template <typename E>
+constexpr int few_wgs() {  // workgroups per CU that the slots leave room for
+  return sizeof(E) == 4 ? 1 : 2;
+}
 template <typename E, bool PAGED>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) void k_attend_few(AttendArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wgs<E>()))) void k_attend_few(AttendArgs a) {
   using L = LE<E>;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float wm[4][kFewRows], wl[4][kFewRows];
@@ -493,7 +640,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) v
   if (!w.any) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 31, h = lane >> 5;
-  char *K = lds + wave * 64 * lds_row<L>(), *V = K + 32 * lds_row<L>();
+  char *K = lds + wave * 64 * lds_row<E>(), *V = K + 32 * lds_row<E>();
+  // the wave's keys: a quarter of the split's, in whole tiles
+  const int quarter = ((w.v_end - w.v_begin + 3) / 4 + 31) & ~31;
+  const int begin = min(w.v_begin + wave * quarter, w.v_end), end = min(begin + quarter, w.v_end);
+  RowCopies<E, PAGED, 32> rc(a.kv, w.km, w.at.b, w.kvh, end);
+  constexpr int NL = decltype(rc)::NL;
+  if (begin < end) {
+    rc.seek(begin);
+    rc.template copy<false, true>(a.kv.k, K, 0);
+    rc.template copy<true, true>(a.kv.v, V, 0);
+  }
   const Row row = tile_row(a, w, r);
   const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
   const Scale scale = score_scale<E>(a, sc);
@@ -501,22 +658,32 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) v
   load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
   const Row first = tile_row(a, w, 0), last = tile_row(a, w, w.rows - 1);
   RowSight see = row.see;
-  see.hi = min(see.hi, w.v_end);
+  see.hi = min(see.hi, end);
+  const int all_hi = min(first.see.hi, end);
 
   RowState st;
   st.m = -kInf;
   st.l = 0.0f;
 #pragma unroll
   for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
-  for (int v0 = w.v_begin + 32 * wave; v0 < w.v_end; v0 += 128) {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    stage_rows<E, PAGED, 32, 64>(a.kv, w.at.b, w.kvh, w.km, v0, w.v_end, lane, K, V);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const bool whole = v0 + 32 <= min(first.see.hi, w.v_end) && (v0 >= last.see.lo || v0 + 32 <= last.see.sv);
-    if (whole) attend_step<L, 1, false>(st, q, K, V, v0, see, scale.c);
-    else attend_step<L, 1, true>(st, q, K, V, v0, see, scale.c);
+  for (int v0 = begin; v0 < end; v0 += 32) {
+    const bool more = v0 + 32 < end;
+    const bool whole = v0 + 32 <= all_hi && (v0 >= last.see.lo || v0 + 32 <= last.see.sv);
+    wait_copies<NL>();
+    af32x16 s[1] = {score_block(q, K, 0, E{})};
+    wait_reads();
+    if (more) {
+      rc.seek(v0 + 32);
+      rc.template copy<false, true>(a.kv.k, K, 0);
+    }
+    if (whole) softmax_step<1, false>(st, s, v0, see, scale.c);
+    else softmax_step<1, true>(st, s, v0, see, scale.c);
+    if (more) wait_copies<NL>();
+    else wait_copies<0>();
+    if (whole) add_values<false>(st, s[0], V, 0, E{});
+    else add_values<true>(st, s[0], V, 0, E{});
+    wait_reads();
+    if (more) rc.template copy<true, true>(a.kv.v, V, 0);
   }
 
   // join the waves: out = sum_w 2^(m_w - m) O_w / sum_w 2^(m_w - m) l_w
@@ -595,9 +762,12 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   else reinterpret_cast<float2 *>(out)[lane] = make_float2(o.x * g, o.y * g);
 }
 
+// Few rows: a K and a V slot of 32 rows per wave, and at the end the waves'
+// outputs.  Many: two tiles of K and of V (FP8: one, the next is in registers).
 template <typename E>
 constexpr size_t attend_lds(bool few) {
-  return few ? (size_t)4 * 64 * lds_row<LE<E>>() : (size_t)2 * many_keys<E>() * lds_row<LE<E>>();
+  const size_t slots = (size_t)4 * 64 * lds_row<E>(), join = (size_t)4 * kFewRows * kHeadDim * 4;
+  return few ? (slots > join ? slots : join) : (size_t)(sizeof(E) == 1 ? 2 : 4) * many_keys<E>() * lds_row<LE<E>>();
 }
 
 template <typename E>
