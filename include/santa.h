@@ -306,9 +306,8 @@ typedef struct {
 
 /* Sliding window with sinks: the token at position p sees position j <= p if
  * j > p - window or j < sinks.  window >= 1 (it counts the token itself),
- * sinks >= 0.  Cache rows that no token of the call sees are not read, nor are
- * their block-table entries, so pages wholly between sinks and window may be
- * freed. */
+ * sinks >= 0.  Cache rows that no token of the call sees are not read, so pages
+ * wholly between sinks and window may be freed. */
 typedef struct {
   int32_t window;
   int32_t sinks;

@@ -16,10 +16,13 @@
 // it scored and V's operand is read from LDS to match (a transposing read for
 // 16-bit elements).  Rescaling a row of O^T is one multiplication per register.
 //
-// Keys.  The keys that a tile's tokens can see are the sinks [0, n0) and a run
-// that ends at its last token; they are numbered v = 0 .. nv - 1 without the
-// gap between, so no tile is spent on hidden keys and rows outside are never
-// touched (their pages may have been freed).
+// Keys.  The keys that a tile's tokens can see are the sinks and a run that
+// ends at its last token; they are numbered v = 0 .. nv - 1 with the hidden gap
+// between left out, so no tile is spent on it.  The numbering keeps positions
+// modulo 16, so that 16 rows from a multiple of 16 on are a run of one page (of
+// 16 keys or more) and need one address; a row of such a group that no token
+// sees is replaced by one that some token does, so hidden rows are never read
+// (their pages may have been freed) and are masked like every other.
 #pragma once
 
 #include "santa_chunk.h"
@@ -38,30 +41,34 @@ typedef float af32x16 __attribute__((ext_vector_type(16)));
 template <typename E>
 using LE = QE<E>;
 
-// Visible keys of a tile: v < n0 is position v, v >= n0 position v + shift.
+// Keys of a tile by number: v < n0 is position v, v >= n0 position v + shift;
+// positions in [sinks, lo) are hidden from all of the tile's tokens.
 struct KeyMap {
-  int n0, shift, nv;
+  int n0, shift, nv, sinks, lo;
   __device__ __forceinline__ int pos(int v) const { return v < n0 ? v : v + shift; }
+  // the position whose row stands in for v's: a visible one
+  __device__ __forceinline__ int row(int v) const {
+    const int p = pos(v);
+    return p >= sinks ? max(p, lo) : p;
+  }
 };
 
 // Tokens at positions p_lo .. p_hi together see [0, sinks) and (p_lo - window, p_hi].
 __device__ __forceinline__ KeyMap key_map(int p_lo, int p_hi, int window, int sinks) {
   const int lo = window ? max(0, p_lo - window + 1) : 0;
-  if (lo <= sinks) return KeyMap{0, 0, p_hi + 1};
-  return KeyMap{sinks, lo - sinks, sinks + p_hi + 1 - lo};
+  const int n0 = (int)min((int64_t)sinks + 15, (int64_t)p_hi + 16) & ~15;
+  if ((lo & ~15) <= n0) return KeyMap{0, 0, p_hi + 1, sinks, lo};
+  const int shift = (lo & ~15) - n0;
+  return KeyMap{n0, shift, p_hi + 1 - shift, sinks, lo};
 }
 
-// What row r of a tile sees, in v: v < hi and (v >= lo or v < sv).
+// What a token sees, in v: v < hi and (v >= lo or v < sv).
 struct RowSight {
   int lo, hi, sv;
 };
-__device__ __forceinline__ RowSight row_sight(const KeyMap &km, int p, int window, int sinks) {
-  RowSight s;
-  const int first = window ? max(0, p - window + 1) : 0;  // the window's first position
-  s.hi = p < km.n0 + km.shift ? min(p + 1, km.n0) : p + 1 - km.shift;
-  s.lo = km.shift ? km.n0 + max(0, first - km.n0 - km.shift) : first;
-  s.sv = km.shift ? km.n0 : min(sinks, km.nv);
-  return s;
+__device__ __forceinline__ RowSight row_sight(const KeyMap &km, int p, int window) {
+  const int first = window ? max(0, p - window + 1) : 0;  // the window's first position, past any gap
+  return RowSight{first - km.shift, p + 1 - km.shift, min(km.sinks, km.nv)};
 }
 
 // Rows in LDS.  L: bfloat16, float32, or FP8 codes as they are in the cache
@@ -222,72 +229,80 @@ __device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int i = 0; i < 8; ++i) pf[b][i] = (__bf16)p[8 * b + i];  // nearest even: 2^-9 of a weight, the sum keeps 32 bits
+  uint32_t bad = 0;
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    uint4 w[2];
-    uint32_t bad = 0;
+  for (int n = 0; n < 4; ++n)
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      w[b] = value_operand(V, 32 * t + 16 * b + 4 * h, n, L{});
-      if constexpr (EDGE)
-        bad |= nonfinite2(w[b].x) | nonfinite2(w[b].y) | nonfinite2(w[b].z) | nonfinite2(w[b].w);
+      uint4 w = value_operand(V, 32 * t + 16 * b + 4 * h, n, L{});
+      if constexpr (EDGE) {
+        const uint4 f = make_uint4(nonfinite2(w.x), nonfinite2(w.y), nonfinite2(w.z), nonfinite2(w.w));
+        bad |= f.x | f.y | f.z | f.w;
+        w = make_uint4(w.x & ~f.x, w.y & ~f.y, w.z & ~f.z, w.w & ~f.w);
+      }
+      st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, w), pf[b], st.o[n], 0, 0, 0);
     }
-    if (EDGE && __any(bad != 0)) {
+  if (EDGE && __any(bad != 0)) {
 #pragma unroll 1
-      for (int kind = 0; kind < 3; ++kind) {
+    for (int kind = 0; kind < 3; ++kind) {
+      const float add = mark_value(kind);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
         af32x16 c = {};
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          const uint4 mk = make_uint4(mark2(w[b].x, kind), mark2(w[b].y, kind), mark2(w[b].z, kind), mark2(w[b].w, kind));
+          const uint4 w = value_operand(V, 32 * t + 16 * b + 4 * h, n, L{});
+          const uint4 mk = make_uint4(mark2(w.x, kind), mark2(w.y, kind), mark2(w.z, kind), mark2(w.w, kind));
           c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, mk), pf[b], c, 0, 0, 0);
         }
-        const float add = mark_value(kind);
 #pragma unroll
         for (int i = 0; i < 16; ++i) st.o[n][i] += c[i] > 0.0f ? add : 0.0f;
       }
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-        w[b] = make_uint4(w[b].x & ~nonfinite2(w[b].x), w[b].y & ~nonfinite2(w[b].y), w[b].z & ~nonfinite2(w[b].z),
-                          w[b].w & ~nonfinite2(w[b].w));
     }
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-      st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, w[b]), pf[b], st.o[n], 0, 0, 0);
   }
 }
 template <bool EDGE, typename L, std::enable_if_t<sizeof(L) == 4, int> = 0>
 __device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, L) {
   const int lane = threadIdx.x & 63, d = lane & 31, h = lane >> 5;
-#pragma unroll
-  for (int n = 0; n < 4; ++n) {
+  auto value = [&](int n, int i) {
     const char *col = V + (32 * t + 4 * h) * lds_row<float>() + (((8 * n + (d >> 2)) ^ (h << 3)) << 4) + (d & 3) * 4;
-    float w[16];
-    bool bad = false;
+    return *reinterpret_cast<const float *>(col + (8 * (i >> 2) + (i & 3)) * lds_row<float>());
+  };
+  bool bad = false;
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      w[i] = *reinterpret_cast<const float *>(col + (8 * (i >> 2) + (i & 3)) * lds_row<float>());
-      if constexpr (EDGE) bad |= !(fabsf(w[i]) < kInf);
+      float w = value(n, i);
+      if constexpr (EDGE) {
+        const bool finite = fabsf(w) < kInf;
+        bad |= !finite;
+        w = finite ? w : 0.0f;
+      }
+      st.o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, p[i], st.o[n], 0, 0, 0);
     }
-    if (EDGE && __any(bad)) {
+  if (EDGE && __any(bad)) {
 #pragma unroll 1
-      for (int kind = 0; kind < 3; ++kind) {
+    for (int kind = 0; kind < 3; ++kind) {
+      const float add = mark_value(kind);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
         af32x16 c = {};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(mark1(w[i], kind), p[i], c, 0, 0, 0);
-        const float add = mark_value(kind);
+        for (int i = 0; i < 16; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(mark1(value(n, i), kind), p[i], c, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) st.o[n][i] += c[i] > 0.0f ? add : 0.0f;
       }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = fabsf(w[i]) < kInf ? w[i] : 0.0f;
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) st.o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], p[i], st.o[n], 0, 0, 0);
   }
 }
 
 // One step of the online softmax: raw scores of NB blocks of 32 keys from
-// number v0 on become weights, and the running state follows.
+// number v0 on become weights, and the running state follows.  The reference m
+// of a row moves only when a score passes it by more than 8 in log2 units: a
+// weight is at most 2^8, which costs 32-bit sums and the weights' rounding
+// nothing, and the output is rescaled in the first tiles only instead of
+// whenever one of 32 rows finds a new maximum.
 template <int NB, bool EDGE>
 __device__ __forceinline__ void softmax_step(RowState &st, af32x16 (&s)[NB], int v0, const RowSight &rs, float c) {
   const int h = (threadIdx.x >> 5) & 1;
@@ -303,10 +318,9 @@ __device__ __forceinline__ void softmax_step(RowState &st, af32x16 (&s)[NB], int
       tm = fmaxf(tm, s[t][i]);
     }
   tm = xor32_max(tm);
-  const float mn = fmaxf(st.m, tm);
-  const float mc = mn == -kInf ? 0.0f : mn * c;  // nothing visible yet: every weight is 0
-  if (__any(mn > st.m)) {
-    const float f = fast_exp2(fmaf(st.m, c, -mc));
+  if (__any(tm * c > fmaf(st.m, c, 8.0f))) {  // (no score yet: -inf, passed by any score but -inf)
+    const float mn = fmaxf(st.m, tm);
+    const float f = mn == -kInf ? 1.0f : fast_exp2((st.m - mn) * c);
     st.l *= f;
 #pragma unroll
     for (int n = 0; n < 4; ++n)
@@ -314,78 +328,118 @@ __device__ __forceinline__ void softmax_step(RowState &st, af32x16 (&s)[NB], int
       for (int i = 0; i < 16; ++i) st.o[n][i] *= f;
     st.m = mn;
   }
+  const float mc = st.m == -kInf ? 0.0f : st.m * c;  // nothing visible yet: every weight is 0
+  float l[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int t = 0; t < NB; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       s[t][i] = fast_exp2(fmaf(s[t][i], c, -mc));
-      st.l += s[t][i];
+      l[i & 1] += s[t][i];
     }
+  st.l += l[0] + l[1];
 }
 
 // ---------------------------------------------------------------------------
 // Cache rows into LDS
 // ---------------------------------------------------------------------------
-// A wave's share of a tile, R consecutive rows: NL copies of 1 KiB, RPL rows
-// each, straight into LDS (no registers in between).  Copy n's lane takes chunk
-// `lane % CPR` of its row as the swizzle moves it, from row n * RPL + lane / CPR.
+// A wave's share of a tile: R rows, copied straight into LDS (no registers in
+// between), RPL rows per copy of 1 KiB.  Copy n's lane takes chunk `lane % CPR`,
+// as the swizzle moves it, of row n * RPL + lane / CPR.  Rows of a multiple of
+// 16 on are one run in memory (see KeyMap), so a copy's address is a uniform
+// base and a lane's constant offset; groups at the ends of what is visible, and
+// pages of fewer than 16 keys, take an address per row.
 template <typename E, bool PAGED, int R>
 struct RowCopies {
   static constexpr int CPR = kHeadDim * (int)sizeof(E) / 16, RPL = 64 / CPR, NL = R / RPL;
-  static_assert(R % RPL == 0, "whole copies");
+  static constexpr int GR = R < 16 ? R : 16, GN = GR / RPL, NG = R / GR;  // rows and copies of a group, groups
+  static_assert(R % RPL == 0 && R % GR == 0 && GR % RPL == 0, "whole copies, whole groups");
   const KvView &kv;
   const KeyMap km;
-  int64_t base;    // elements to the sequence's (contiguous) or the pool's (paged) KV head
-  int b, end;      // rows at or past `end` repeat the last one before it
-  int win, first, upto;  // paged: lane i holds the sequence's table entry first + i, up to `upto`
-  int64_t at[NL];  // byte offsets of the rows of the tile that is copied next
+  int64_t base;         // elements to the sequence's (contiguous) or the pool's (paged) KV head
+  int b, end, row0;     // rows at or past `end` repeat the last one before it; row0: the share's row in the tile
+  int win, nxt, first;  // paged: lane i holds the sequence's table entries first + i and first + 64 + i
+  int last_entry;       // (table entries past the last key's are not read)
+  uint32_t lane_off;    // the lane's row within a copy, in bytes
+  int v0;
+  bool runs;            // every group of them is a run; otherwise they take an address per row
+  uint64_t at[NG];      // byte offset of each group's first row
 
-  __device__ __forceinline__ RowCopies(const KvView &kv_, const KeyMap &km_, int b_, int kvh, int end_)
-      : kv(kv_), km(km_), b(b_), end(end_), win(0), first(0), upto(-1) {
+  __device__ __forceinline__ RowCopies(const KvView &kv_, const KeyMap &km_, int b_, int kvh, int end_, int row0_)
+      : kv(kv_), km(km_), b(b_), end(end_), row0(row0_), win(0), nxt(0), first(-256) {
     base = (int64_t)kvh * kv.sh + (PAGED ? 0 : (int64_t)b * kv.sb);
+    lane_off = (uint32_t)((int64_t)((threadIdx.x & 63) / CPR) * kv.sn * (int64_t)sizeof(E));
+    last_entry = PAGED && end > 0 ? km.row(end - 1) >> kv.ps_log2 : 0;
   }
-  __device__ __forceinline__ static int row_of(int n) { return n * RPL + (threadIdx.x & 63) / CPR; }
+  __device__ __forceinline__ int entry(int i) const {
+    return kv.bt[(int64_t)b * kv.max_pages + min(i + (int)(threadIdx.x & 63), last_entry)];
+  }
 
-  // The rows from key v0 on (v0 < end) are next.
-  __device__ __forceinline__ void seek(int v0) {
-    if constexpr (PAGED) {
-      const int last = min(v0 + R, end) - 1;
-      const int e0 = km.pos(v0) >> kv.ps_log2, e1 = km.pos(last) >> kv.ps_log2;
-      const bool gap = v0 < km.n0 && last >= km.n0;  // sinks and window in one tile: entries far apart
-      if (!gap && (e0 < first || e1 > upto)) {
-        first = e0;
-        upto = min(e0 + 63, km.pos((v0 < km.n0 ? min(km.n0, end) : end) - 1) >> kv.ps_log2);  // the run's last key
-        win = kv.bt[(int64_t)b * kv.max_pages + min(e0 + (int)(threadIdx.x & 63), upto)];
-      }
+  // The rows from key v on are next (some of the tile's keys lie before `end`).
+  __device__ __forceinline__ void seek(int v) {
+    v0 = v;
+    runs = v + R <= end && (!PAGED || kv.ps_log2 >= 4);
 #pragma unroll
-      for (int n = 0; n < NL; ++n) {
-        const int pos = km.pos(min(v0 + row_of(n), end - 1)), e = pos >> kv.ps_log2;
-        const int page = gap ? kv.bt[(int64_t)b * kv.max_pages + e] : __shfl(win, e - first);
-        at[n] = (base + (int64_t)page * kv.sb + (int64_t)(pos & ((1 << kv.ps_log2) - 1)) * kv.sn) * (int64_t)sizeof(E);
-      }
-    } else {
+    for (int g = 0; g < NG; ++g) {
+      const int p = km.pos(v + g * GR);
+      runs = runs && (p >= km.lo || p + GR <= km.sinks);
+    }
+    if (!runs) return;
 #pragma unroll
-      for (int n = 0; n < NL; ++n)
-        at[n] = (base + (int64_t)km.pos(min(v0 + row_of(n), end - 1)) * kv.sn) * (int64_t)sizeof(E);
+    for (int g = 0; g < NG; ++g) {
+      const int p = km.pos(v + g * GR);
+      if constexpr (PAGED) {
+        const int e = p >> kv.ps_log2;
+        if (e < first || e >= first + 64) {  // the next 64 entries are fetched 64 entries ahead of their use
+          const bool ahead = e >= first + 64 && e < first + 128;
+          first = ahead ? first + 64 : e;
+          win = ahead ? nxt : entry(first);
+          nxt = entry(first + 64);
+        }
+        const int page = __builtin_amdgcn_readlane(win, e - first);
+        at[g] = (uint64_t)((base + (int64_t)page * kv.sb + (int64_t)(p & ((1 << kv.ps_log2) - 1)) * kv.sn) *
+                           (int64_t)sizeof(E));
+      } else {
+        at[g] = (uint64_t)((base + (int64_t)p * kv.sn) * (int64_t)sizeof(E));
+      }
     }
   }
 
-  // Start copying the rows of `src` (kv.k or kv.v) to LDS rows row0 .. of `dst`.
+  // Start copying the rows of `src` (kv.k or kv.v) into the LDS tile at `dst`.
   // NT: read once by the whole call, so that they do not displace other lines.
   template <bool VALUES, bool NT>
-  __device__ __forceinline__ void copy(const void *src, char *dst, int row0) const {
+  __device__ __forceinline__ void copy(const void *src, char *dst) const {
     const unsigned m = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_addr(dst + row0 * lds_row<E>()));
-    const int p = (threadIdx.x & 63) % CPR;
+    const int lane = threadIdx.x & 63;
+    auto chunk = [&](int row) {
+      return (lane % CPR) ^ (VALUES ? v_swz<E>(row0 + row) : k_swz<E>(row0 + row));
+    };
+    if (runs) {
 #pragma unroll
-    for (int n = 0; n < NL; ++n) {
-      const int row = row0 + row_of(n), ch = p ^ (VALUES ? v_swz<E>(row) : k_swz<E>(row));
-      const char *g = static_cast<const char *>(src) + at[n] + ch * 16;
-      if constexpr (NT)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
-                     ::"s"(m + n * 1024u), "v"(g) : "memory", "m0");
-      else
+      for (int n = 0; n < NL; ++n) {
+        const char *s = static_cast<const char *>(src) + at[n / GN] + (uint64_t)(n % GN * RPL) * (uint64_t)kv.sn * sizeof(E);
+        const uint32_t o = lane_off + chunk(n * RPL + lane / CPR) * 16;
+        if constexpr (NT)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                       ::"s"(m + n * 1024u), "v"(o), "s"(s) : "memory", "m0");
+        else
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                       ::"s"(m + n * 1024u), "v"(o), "s"(s) : "memory", "m0");
+      }
+    } else {
+#pragma unroll 1
+      for (int n = 0; n < NL; ++n) {
+        const int row = n * RPL + lane / CPR, p = km.row(min(v0 + row, end - 1));
+        int64_t off = base;
+        if constexpr (PAGED)
+          off += (int64_t)kv.bt[(int64_t)b * kv.max_pages + (p >> kv.ps_log2)] * kv.sb +
+                 (int64_t)(p & ((1 << kv.ps_log2) - 1)) * kv.sn;
+        else
+          off += (int64_t)p * kv.sn;
+        const char *s = static_cast<const char *>(src) + off * (int64_t)sizeof(E) + chunk(row) * 16;
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                     ::"s"(m + n * 1024u), "v"(g) : "memory", "m0");
+                     ::"s"(m + n * 1024u), "v"(s) : "memory", "m0");
+      }
     }
   }
 };
@@ -408,7 +462,7 @@ struct WidenedRows {
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
       const int i = n * kThreads + threadIdx.x;
-      const int64_t off = row_offset<PAGED>(kv, b, kvh, km.pos(min(v0 + i / 8, end - 1))) + (i % 8) * 16;
+      const int64_t off = row_offset<PAGED>(kv, b, kvh, km.row(min(v0 + i / 8, end - 1))) + (i % 8) * 16;
       k[n] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(kv.k) + off);
       v[n] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(kv.v) + off);
     }
@@ -447,19 +501,26 @@ __device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile
   w.kvh = (int)(id % a.Hkv);
   w.t = (int)(id / a.Hkv % a.T);
   const int64_t x = a.tiles - 1 - id / a.Hkv / a.T;
-  w.at = find_tile(a.ch, x, a.tile_tokens);
+  const TileAt at = find_tile(a.ch, x, a.tile_tokens);
+  auto uniform = [](int i) { return __builtin_amdgcn_readfirstlane(i); };
+  w.at = TileAt{uniform(at.b), uniform(at.first), uniform(at.count), uniform(at.i0)};
   w.any = w.at.b < a.ch.B;
   w.out_row = ((x * a.Hkv + w.kvh) * a.T + w.t) * rows_per_tile;
   if (!w.any) return w;
-  const int L = seq_len(a.kv, w.at.b), n = min(a.tile_tokens, w.at.count - w.at.i0);
+  const int L = uniform(seq_len(a.kv, w.at.b)), n = min(a.tile_tokens, w.at.count - w.at.i0);
   w.rows = n * a.G;
   w.p_lo = L - w.at.count + w.at.i0;
   // (a chunk longer than its context: tokens before position 0 see nothing)
-  w.km = w.p_lo + n - 1 < 0 ? KeyMap{0, 0, 0} : key_map(max(w.p_lo, 0), w.p_lo + n - 1, a.window, a.sinks);
+  w.km = w.p_lo + n - 1 < 0 ? KeyMap{0, 0, 0, 0, 0} : key_map(max(w.p_lo, 0), w.p_lo + n - 1, a.window, a.sinks);
   const int len = ((w.km.nv + a.T - 1) / a.T + a.step - 1) / a.step * a.step;
   w.v_begin = min(w.t * len, w.km.nv);
   w.v_end = min(w.v_begin + len, w.km.nv);
   return w;
+}
+
+__device__ __forceinline__ RowSight tile_sight(const AttendArgs &a, const Work &w, int r) {
+  const int p = w.p_lo + r / a.G;
+  return p < 0 ? RowSight{0, 0, 0} : row_sight(w.km, p, a.window);
 }
 
 // Row r of the tile: its query row, and what it sees.  Rows past the last see
@@ -474,8 +535,7 @@ __device__ __forceinline__ Row tile_row(const AttendArgs &a, const Work &w, int 
   x.valid = r < w.rows;
   const int rr = min(r, w.rows - 1), i = rr / a.G;
   x.at = ((int64_t)(w.at.first + w.at.i0 + i) * a.Hq + w.kvh * a.G + rr % a.G) * kHeadDim;
-  const int p = w.p_lo + i;
-  x.see = p < 0 ? RowSight{0, 0, 0} : row_sight(w.km, p, a.window, a.sinks);
+  x.see = tile_sight(a, w, rr);
   return x;
 }
 
@@ -522,39 +582,30 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const Scale scale = score_scale<E>(a, sc);
   AQ<L> q;
   load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
-  // what all of the wave's rows see, and what any of them does
-  const bool live = 32 * wave < w.rows;
-  const Row first = tile_row(a, w, 32 * wave), last = tile_row(a, w, min(32 * wave + 31, w.rows - 1));
+  // a tile is whole if every row sees all of its keys
+  const RowSight first = tile_sight(a, w, 0), last = tile_sight(a, w, w.rows - 1);
+  const int all_hi = min(first.hi, w.v_end);
   RowSight see = row.see;
   see.hi = min(see.hi, w.v_end);
-  const int all_hi = min(first.see.hi, w.v_end);
 
   RowState st;
   st.m = -kInf;
   st.l = 0.0f;
 #pragma unroll
   for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
-  // (the wave has no share in a tile that none of its rows see)
   auto step = [&](int v0, const char *K, const char *V, auto between) {
-    const bool mine = live && v0 < last.see.hi && (v0 + KEYS > first.see.lo || v0 < first.see.sv);
-    const bool whole = v0 + KEYS <= all_hi && (v0 >= last.see.lo || v0 + KEYS <= last.see.sv);
-    af32x16 s[NB];
-    if (mine) {
+    auto body = [&](auto edge) {
+      constexpr bool EDGE = decltype(edge)::value;
+      af32x16 s[NB];
 #pragma unroll
       for (int t = 0; t < NB; ++t) s[t] = score_block(q, K, t, L{});
-      if (whole) softmax_step<NB, false>(st, s, v0, see, scale.c);
-      else softmax_step<NB, true>(st, s, v0, see, scale.c);
-    }
-    between();
-    if (mine) {
-      if (whole) {
+      softmax_step<NB, EDGE>(st, s, v0, see, scale.c);
+      between();
 #pragma unroll
-        for (int t = 0; t < NB; ++t) add_values<false>(st, s[t], V, t, L{});
-      } else {
-#pragma unroll
-        for (int t = 0; t < NB; ++t) add_values<true>(st, s[t], V, t, L{});
-      }
-    }
+      for (int t = 0; t < NB; ++t) add_values<EDGE>(st, s[t], V, t, L{});
+    };
+    if (v0 + KEYS <= all_hi && (v0 >= last.lo || v0 + KEYS <= last.sv)) body(std::false_type{});
+    else body(std::true_type{});
   };
   if constexpr (WIDEN) {
     WidenedRows<PAGED, KEYS> next;
@@ -569,13 +620,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
   } else {
     constexpr int R = KEYS / 4;
-    RowCopies<E, PAGED, R> rc(a.kv, w.km, w.at.b, w.kvh, w.v_end);
-    const int r0 = R * wave;
-    auto begin = [&](int v0) { rc.seek(min(v0 + r0, w.v_end - 1)); };
+    RowCopies<E, PAGED, R> rc(a.kv, w.km, w.at.b, w.kvh, w.v_end, R * wave);
     if (w.v_begin < w.v_end) {
-      begin(w.v_begin);
-      rc.template copy<false, false>(a.kv.k, lds, r0);
-      rc.template copy<true, false>(a.kv.v, lds + 2 * TB, r0);
+      rc.seek(w.v_begin + R * wave);
+      rc.template copy<false, false>(a.kv.k, lds);
+      rc.template copy<true, false>(a.kv.v, lds + 2 * TB);
     }
     int turn = 0;
     for (int v0 = w.v_begin; v0 < w.v_end; v0 += KEYS) {
@@ -586,14 +635,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       wait_copies<decltype(rc)::NL>();
       __syncthreads();
       if (more) {
-        begin(v0 + KEYS);
-        rc.template copy<false, false>(a.kv.k, lds + (turn ^ 1) * TB, r0);
+        rc.seek(v0 + KEYS + R * wave);
+        rc.template copy<false, false>(a.kv.k, lds + (turn ^ 1) * TB);
       }
       step(v0, K, V, [&] {
         if (more) wait_copies<decltype(rc)::NL>();
         else wait_copies<0>();
         __syncthreads();
-        if (more) rc.template copy<true, false>(a.kv.v, lds + (2 + (turn ^ 1)) * TB, r0);
+        if (more) rc.template copy<true, false>(a.kv.v, lds + (2 + (turn ^ 1)) * TB);
       });
       turn ^= 1;
     }
@@ -644,22 +693,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   // the wave's keys: a quarter of the split's, in whole tiles
   const int quarter = ((w.v_end - w.v_begin + 3) / 4 + 31) & ~31;
   const int begin = min(w.v_begin + wave * quarter, w.v_end), end = min(begin + quarter, w.v_end);
-  RowCopies<E, PAGED, 32> rc(a.kv, w.km, w.at.b, w.kvh, end);
+  RowCopies<E, PAGED, 32> rc(a.kv, w.km, w.at.b, w.kvh, end, 0);
   constexpr int NL = decltype(rc)::NL;
   if (begin < end) {
     rc.seek(begin);
-    rc.template copy<false, true>(a.kv.k, K, 0);
-    rc.template copy<true, true>(a.kv.v, V, 0);
+    rc.template copy<false, true>(a.kv.k, K);
+    rc.template copy<true, true>(a.kv.v, V);
   }
   const Row row = tile_row(a, w, r);
   const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
   const Scale scale = score_scale<E>(a, sc);
   AQ<L> q;
   load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
-  const Row first = tile_row(a, w, 0), last = tile_row(a, w, w.rows - 1);
+  const RowSight first = tile_sight(a, w, 0), last = tile_sight(a, w, w.rows - 1);
   RowSight see = row.see;
   see.hi = min(see.hi, end);
-  const int all_hi = min(first.see.hi, end);
+  const int all_hi = min(first.hi, end);
 
   RowState st;
   st.m = -kInf;
@@ -668,22 +717,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
   for (int v0 = begin; v0 < end; v0 += 32) {
     const bool more = v0 + 32 < end;
-    const bool whole = v0 + 32 <= all_hi && (v0 >= last.see.lo || v0 + 32 <= last.see.sv);
     wait_copies<NL>();
     af32x16 s[1] = {score_block(q, K, 0, E{})};
     wait_reads();
     if (more) {
       rc.seek(v0 + 32);
-      rc.template copy<false, true>(a.kv.k, K, 0);
+      rc.template copy<false, true>(a.kv.k, K);
     }
-    if (whole) softmax_step<1, false>(st, s, v0, see, scale.c);
-    else softmax_step<1, true>(st, s, v0, see, scale.c);
-    if (more) wait_copies<NL>();
-    else wait_copies<0>();
-    if (whole) add_values<false>(st, s[0], V, 0, E{});
-    else add_values<true>(st, s[0], V, 0, E{});
+    auto rest = [&](auto edge) {
+      constexpr bool EDGE = decltype(edge)::value;
+      softmax_step<1, EDGE>(st, s, v0, see, scale.c);
+      if (more) wait_copies<NL>();
+      else wait_copies<0>();
+      add_values<EDGE>(st, s[0], V, 0, E{});
+    };
+    if (v0 + 32 <= all_hi && (v0 >= last.lo || v0 + 32 <= last.sv)) rest(std::false_type{});
+    else rest(std::true_type{});
     wait_reads();
-    if (more) rc.template copy<true, true>(a.kv.v, V, 0);
+    if (more) rc.template copy<true, true>(a.kv.v, V);
   }
 
   // join the waves: out = sum_w 2^(m_w - m) O_w / sum_w 2^(m_w - m) l_w
