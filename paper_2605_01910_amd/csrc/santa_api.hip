@@ -303,7 +303,7 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
   p.step = p.few || p.elem == 1 ? 32 : 64;
   // about two workgroups per CU, none with fewer keys than its start costs
   const int64_t groups = p.tiles * p.Hkv;
-  int64_t T = std::min<int64_t>(512 / groups, p.few ? (keys + 127) / 128 : keys / 256);
+  int64_t T = std::min<int64_t>(512 / groups, (keys + (p.elem == 1 ? 63 : 127)) / (p.elem == 1 ? 64 : 128));
   if (g_opts.splits > 0) T = g_opts.splits;
   p.T = (int)std::max<int64_t>(1, std::min<int64_t>(T, santa::kMaxSplits));
   size_t off = 0;

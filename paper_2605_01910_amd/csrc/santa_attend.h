@@ -123,45 +123,58 @@ __device__ __forceinline__ void load_rows(AQ<float> &q, const float *p, bool val
   }
 }
 
-// Scores of keys [32 t, 32 t + 32) of the tile at K, raw (before the scale).
-__device__ __forceinline__ af32x16 score_block(const AQ<uint16_t> &q, const char *K, int t, uint8_t) {
+// Raw scores (before the scale) of the tile's NB blocks of 32 keys with H blocks
+// of 32 rows: a key operand read from LDS once serves all H.
+template <int H, int NB>
+__device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<uint16_t> (&q)[H], const char *K, uint8_t) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-  const char *row = K + (32 * t + r) * lds_row<uint8_t>() + 8 * h;
+  const char *row = K + r * lds_row<uint8_t>() + 8 * h;
   const int x = (r >> 1) & 7;
-  af32x16 s = {};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const Chunk<uint8_t> k{*reinterpret_cast<const uint2 *>(row + ((i ^ x) << 4))};
-    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, k.to_bf16()), q.f[i], s, 0, 0, 0);
-  }
-  return s;
+  for (int t = 0; t < NB; ++t)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const Chunk<uint8_t> k{*reinterpret_cast<const uint2 *>(row + 32 * t * lds_row<uint8_t>() + ((i ^ x) << 4))};
+      const abf16x8 k16 = __builtin_bit_cast(abf16x8, k.to_bf16());
+#pragma unroll
+      for (int c = 0; c < H; ++c)
+        s[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k16, q[c].f[i], i ? s[c][t] : af32x16{}, 0, 0, 0);
+    }
 }
-__device__ __forceinline__ af32x16 score_block(const AQ<uint16_t> &q, const char *K, int t, uint16_t) {
+template <int H, int NB>
+__device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<uint16_t> (&q)[H], const char *K, uint16_t) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-  const char *row = K + (32 * t + r) * lds_row<uint16_t>();
+  const char *row = K + r * lds_row<uint16_t>();
   const int x = h ^ (r & 15);
-  af32x16 s = {};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const abf16x8 k = *reinterpret_cast<const abf16x8 *>(row + (((2 * i) ^ x) << 4));
-    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q.f[i], s, 0, 0, 0);
-  }
-  return s;
+  for (int t = 0; t < NB; ++t)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const abf16x8 k = *reinterpret_cast<const abf16x8 *>(row + 32 * t * lds_row<uint16_t>() + (((2 * i) ^ x) << 4));
+#pragma unroll
+      for (int c = 0; c < H; ++c)
+        s[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c].f[i], i ? s[c][t] : af32x16{}, 0, 0, 0);
+    }
 }
-__device__ __forceinline__ af32x16 score_block(const AQ<float> &q, const char *K, int t, float) {
+template <int H, int NB>
+__device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<float> (&q)[H], const char *K, float) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-  const char *row = K + (32 * t + r) * lds_row<float>();
+  const char *row = K + r * lds_row<float>();
   const int x = h ^ (r & 15);
-  af32x16 s = {};
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float4 k = *reinterpret_cast<const float4 *>(row + (((2 * i) ^ x) << 4));
-    s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, q.f[i].x, s, 0, 0, 0);
-    s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, q.f[i].y, s, 0, 0, 0);
-    s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, q.f[i].z, s, 0, 0, 0);
-    s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, q.f[i].w, s, 0, 0, 0);
-  }
-  return s;
+  for (int t = 0; t < NB; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float4 k = *reinterpret_cast<const float4 *>(row + 32 * t * lds_row<float>() + (((2 * i) ^ x) << 4));
+#pragma unroll
+      for (int c = 0; c < H; ++c) {
+        af32x16 y = i ? s[c][t] : af32x16{};
+        y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, q[c].f[i].x, y, 0, 0, 0);
+        y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, q[c].f[i].y, y, 0, 0, 0);
+        y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, q[c].f[i].z, y, 0, 0, 0);
+        s[c][t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, q[c].f[i].w, y, 0, 0, 0);
+      }
+    }
 }
 
 // The running state of 32 rows in a wave: maximum (raw score units, the same
@@ -197,137 +210,151 @@ __device__ __forceinline__ uint4 value_operand(const char *V, int row, int n, ui
   return Chunk<uint8_t>{make_uint2((unsigned)w[0], (unsigned)w[1])}.to_bf16();
 }
 
-// Non-finite values stand apart: a key that some rows of the tile do not see
-// must not reach them as 0 * inf.  clean: the operand with those elements 0;
-// mark: 1 where the element is of the kind (0: +inf, 1: -inf, 2: NaN).
-__device__ __forceinline__ uint32_t nonfinite2(uint32_t w) {  // 0xffff halves where exponent is all ones
+// 32-bit values as an operand: feature 32 n + l % 32 of the key of accumulator i.
+__device__ __forceinline__ float value32(const char *V, int t, int n, int i) {
+  const int lane = threadIdx.x & 63, d = lane & 31, h = lane >> 5;
+  const char *col = V + (32 * t + 4 * h) * lds_row<float>() + (((8 * n + (d >> 2)) ^ (h << 3)) << 4) + (d & 3) * 4;
+  return *reinterpret_cast<const float *>(col + (8 * (i >> 2) + (i & 3)) * lds_row<float>());
+}
+
+// Bits of the non-finite elements of two bfloat16.
+__device__ __forceinline__ uint32_t nonfinite2(uint32_t w) {
   const uint32_t e = w & 0x7f807f80u;
   return ((e & 0xffffu) == 0x7f80u ? 0xffffu : 0u) | ((e >> 16) == 0x7f80u ? 0xffff0000u : 0u);
 }
-__device__ __forceinline__ uint32_t mark2(uint32_t w, int kind) {
-  auto one = [&](uint32_t x) {
-    const bool inf = (x & 0x7fffu) == 0x7f80u, nan = (x & 0x7fffu) > 0x7f80u;
-    return (kind == 2 ? nan : inf && ((x >> 15) != 0) == (kind == 1)) ? 0x3f80u : 0u;
-  };
-  return one(w & 0xffffu) | one(w >> 16) << 16;
-}
-__device__ __forceinline__ float mark1(float x, int kind) {
-  const bool nan = x != x;
-  return (kind == 2 ? nan : x == (kind ? -kInf : kInf)) ? 1.0f : 0.0f;
-}
-__device__ __forceinline__ float mark_value(int kind) {
-  return kind == 0 ? kInf : kind == 1 ? -kInf : __builtin_nanf("");
-}
 
-// O^T += V^T P^T over keys [32 t, 32 t + 32) of the tile at V (rows of type L).
-// EDGE: some row may not see some of the keys (their weights are 0).
-template <bool EDGE, typename L, std::enable_if_t<sizeof(L) <= 2, int> = 0>
-__device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, L) {
-  const int h = (threadIdx.x >> 5) & 1;
-  abf16x8 pf[2];
+// The weights of H blocks of rows over NB blocks of keys, as operands.
+template <typename L, int H, int NB>
+struct Weights {
+  abf16x8 f[H][2 * NB];  // nearest even: half a step is 2^-9 of a weight; the sum of weights keeps 32 bits
+};
+template <int H, int NB>
+struct Weights<float, H, NB> {
+  af32x16 f[H][NB];
+};
+
+// O^T += V^T P^T over the tile at V (rows of type L).
+template <typename L, int H, int NB>
+__device__ __forceinline__ void add_values(RowState (&st)[H], const Weights<QE<L>, H, NB> &p, const char *V, L) {
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  if constexpr (sizeof(L) <= 2) {
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) pf[b][i] = (__bf16)p[8 * b + i];  // nearest even: 2^-9 of a weight, the sum keeps 32 bits
-  uint32_t bad = 0;
-#pragma unroll
-  for (int n = 0; n < 4; ++n)
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      uint4 w = value_operand(V, 32 * t + 16 * b + 4 * h, n, L{});
-      if constexpr (EDGE) {
-        const uint4 f = make_uint4(nonfinite2(w.x), nonfinite2(w.y), nonfinite2(w.z), nonfinite2(w.w));
-        bad |= f.x | f.y | f.z | f.w;
-        w = make_uint4(w.x & ~f.x, w.y & ~f.y, w.z & ~f.z, w.w & ~f.w);
-      }
-      st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, w), pf[b], st.o[n], 0, 0, 0);
-    }
-  if (EDGE && __any(bad != 0)) {
-#pragma unroll 1
-    for (int kind = 0; kind < 3; ++kind) {
-      const float add = mark_value(kind);
+    for (int b = 0; b < 2 * NB; ++b)
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        af32x16 c = {};
+        const abf16x8 w = __builtin_bit_cast(abf16x8, value_operand(V, 16 * b + 4 * h, n, L{}));
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint4 w = value_operand(V, 32 * t + 16 * b + 4 * h, n, L{});
-          const uint4 mk = make_uint4(mark2(w.x, kind), mark2(w.y, kind), mark2(w.z, kind), mark2(w.w, kind));
-          c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, mk), pf[b], c, 0, 0, 0);
+        for (int c = 0; c < H; ++c)
+          st[c].o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p.f[c][b], st[c].o[n], 0, 0, 0);
+      }
+  } else {
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float w = value32(V, t, n, i);
+#pragma unroll
+          for (int c = 0; c < H; ++c)
+            st[c].o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, p.f[c][t][i], st[c].o[n], 0, 0, 0);
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st.o[n][i] += c[i] > 0.0f ? add : 0.0f;
-      }
-    }
-  }
-}
-template <bool EDGE, typename L, std::enable_if_t<sizeof(L) == 4, int> = 0>
-__device__ __forceinline__ void add_values(RowState &st, const af32x16 &p, const char *V, int t, L) {
-  const int lane = threadIdx.x & 63, d = lane & 31, h = lane >> 5;
-  auto value = [&](int n, int i) {
-    const char *col = V + (32 * t + 4 * h) * lds_row<float>() + (((8 * n + (d >> 2)) ^ (h << 3)) << 4) + (d & 3) * 4;
-    return *reinterpret_cast<const float *>(col + (8 * (i >> 2) + (i & 3)) * lds_row<float>());
-  };
-  bool bad = false;
-#pragma unroll
-  for (int n = 0; n < 4; ++n)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float w = value(n, i);
-      if constexpr (EDGE) {
-        const bool finite = fabsf(w) < kInf;
-        bad |= !finite;
-        w = finite ? w : 0.0f;
-      }
-      st.o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, p[i], st.o[n], 0, 0, 0);
-    }
-  if (EDGE && __any(bad)) {
-#pragma unroll 1
-    for (int kind = 0; kind < 3; ++kind) {
-      const float add = mark_value(kind);
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        af32x16 c = {};
-#pragma unroll
-        for (int i = 0; i < 16; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(mark1(value(n, i), kind), p[i], c, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st.o[n][i] += c[i] > 0.0f ? add : 0.0f;
-      }
-    }
   }
 }
 
-// One step of the online softmax: raw scores of NB blocks of 32 keys from
-// number v0 on become weights, and the running state follows.  The reference m
-// of a row moves only when a score passes it by more than 8 in log2 units: a
-// weight is at most 2^8, which costs 32-bit sums and the weights' rounding
-// nothing, and the output is rescaled in the first tiles only instead of
-// whenever one of 32 rows finds a new maximum.
-template <int NB, bool EDGE>
-__device__ __forceinline__ void softmax_step(RowState &st, af32x16 (&s)[NB], int v0, const RowSight &rs, float c) {
+// Non-finite values stand apart: a key that some rows of a tile do not see must
+// not reach them as 0 * inf.  In a tile that not all rows see whole, zeros take
+// their place in LDS (clean_values), and add_nonfinite gives them at the end to
+// the rows that do see them.
+// Whether words w hold a non-finite element, and the words with those zeroed.
+__device__ __forceinline__ bool clean_words(uint4 &w, uint16_t) {
+  const uint4 f = make_uint4(nonfinite2(w.x), nonfinite2(w.y), nonfinite2(w.z), nonfinite2(w.w));
+  w = make_uint4(w.x & ~f.x, w.y & ~f.y, w.z & ~f.z, w.w & ~f.w);
+  return (f.x | f.y | f.z | f.w) != 0;
+}
+__device__ __forceinline__ bool clean_words(uint4 &w, float) {
+  bool bad = false;
+  auto one = [&](uint32_t &x) {
+    const bool b = (x & 0x7f800000u) == 0x7f800000u;
+    bad |= b;
+    x = b ? 0u : x;
+  };
+  one(w.x), one(w.y), one(w.z), one(w.w);
+  return bad;
+}
+__device__ __forceinline__ bool clean_words(uint4 &w, uint8_t) {  // E4M3: NaN is the only one
+  bool bad = false;
+  auto one = [&](uint32_t &x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t m = 0x7fu << (8 * i);
+      if ((x & m) == m) {
+        bad = true;
+        x &= ~(0xffu << (8 * i));
+      }
+    }
+  };
+  one(w.x), one(w.y), one(w.z), one(w.w);
+  return bad;
+}
+// Over `bytes` of V by a team of TEAM lanes; whether there were any.
+template <typename L, int TEAM>
+__device__ __forceinline__ bool clean_values(char *V, int bytes, int tl) {
+  bool bad = false;
+#pragma unroll 1
+  for (int i = tl * 16; i < bytes; i += TEAM * 16) {
+    uint4 w = *reinterpret_cast<const uint4 *>(V + i);
+    if (clean_words(w, L{})) {
+      *reinterpret_cast<uint4 *>(V + i) = w;
+      bad = true;
+    }
+  }
+  return bad;
+}
+
+// The online softmax, in three parts.  The reference m of a row moves only when
+// a score passes it by more than 8 in log2 units: a weight is at most 2^8, which
+// costs 32-bit sums and the weights' rounding nothing, and the output is
+// rescaled in the first tiles only instead of whenever one of 32 rows finds a
+// new maximum.
+template <int NB>
+__device__ __forceinline__ void hide(af32x16 (&s)[NB], int v0, const RowSight &rs) {
   const int h = (threadIdx.x >> 5) & 1;
-  float tm = -kInf;
 #pragma unroll
   for (int t = 0; t < NB; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      if constexpr (EDGE) {
-        const int v = v0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3);
-        if (!(v < rs.hi && (v >= rs.lo || v < rs.sv))) s[t][i] = -kInf;
-      }
-      tm = fmaxf(tm, s[t][i]);
+      const int v = v0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3);
+      if (!(v < rs.hi && (v >= rs.lo || v < rs.sv))) s[t][i] = -kInf;
     }
-  tm = xor32_max(tm);
-  if (__any(tm * c > fmaf(st.m, c, 8.0f))) {  // (no score yet: -inf, passed by any score but -inf)
-    const float mn = fmaxf(st.m, tm);
-    const float f = mn == -kInf ? 1.0f : fast_exp2((st.m - mn) * c);
-    st.l *= f;
+}
+template <int NB>
+__device__ __forceinline__ float row_max(const af32x16 (&s)[NB]) {
+  float tm = -kInf;
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+  for (int t = 0; t < NB; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) st.o[n][i] *= f;
-    st.m = mn;
-  }
+    for (int i = 0; i < 16; ++i) tm = fmaxf(tm, s[t][i]);
+  return xor32_max(tm);
+}
+// The factor that the output and the sum so far take (1 if the reference stays;
+// no score yet: m is -inf, passed by any score but -inf).
+__device__ __forceinline__ float move_reference(RowState &st, float tm, float c) {
+  const bool move = tm * c > fmaf(st.m, c, 8.0f);
+  const float f = move ? fast_exp2((st.m - tm) * c) : 1.0f;
+  st.m = move ? tm : st.m;
+  st.l *= f;
+  return f;
+}
+__device__ __forceinline__ void rescale(RowState &st, float f) {
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st.o[n][i] *= f;
+}
+// Scores become weights, and their sum the row's.
+template <int NB>
+__device__ __forceinline__ void weigh(RowState &st, af32x16 (&s)[NB], float c) {
   const float mc = st.m == -kInf ? 0.0f : st.m * c;  // nothing visible yet: every weight is 0
   float l[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -338,6 +365,22 @@ __device__ __forceinline__ void softmax_step(RowState &st, af32x16 (&s)[NB], int
       l[i & 1] += s[t][i];
     }
   st.l += l[0] + l[1];
+}
+template <int H, int NB>
+__device__ __forceinline__ void pack(Weights<uint16_t, H, NB> &w, const af32x16 (&s)[H][NB]) {
+#pragma unroll
+  for (int c = 0; c < H; ++c)
+#pragma unroll
+    for (int b = 0; b < 2 * NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w.f[c][b][i] = (__bf16)s[c][b / 2][8 * (b & 1) + i];
+}
+template <int H, int NB>
+__device__ __forceinline__ void pack(Weights<float, H, NB> &w, const af32x16 (&s)[H][NB]) {
+#pragma unroll
+  for (int c = 0; c < H; ++c)
+#pragma unroll
+    for (int t = 0; t < NB; ++t) w.f[c][t] = s[c][t];
 }
 
 // ---------------------------------------------------------------------------
@@ -452,35 +495,6 @@ __device__ __forceinline__ void wait_copies() {
 // Every LDS read of the wave has returned: what it read may be overwritten.
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// FP8 rows of a full tile: codes through registers, widened on the way into LDS,
-// once for the four waves.  NC: 16-byte chunks of K and of V per lane.
-template <bool PAGED, int KEYS>
-struct WidenedRows {
-  static constexpr int NC = KEYS * 8 / kThreads;
-  uint4 k[NC], v[NC];
-  __device__ __forceinline__ void load(const KvView &kv, const KeyMap &km, int b, int kvh, int v0, int end) {
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      const int i = n * kThreads + threadIdx.x;
-      const int64_t off = row_offset<PAGED>(kv, b, kvh, km.row(min(v0 + i / 8, end - 1))) + (i % 8) * 16;
-      k[n] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(kv.k) + off);
-      v[n] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(kv.v) + off);
-    }
-  }
-  __device__ __forceinline__ void store(char *K, char *V) const {
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      const int i = n * kThreads + threadIdx.x, row = i / 8, c = 2 * (i % 8);
-      char *kd = K + row * lds_row<uint16_t>(), *vd = V + row * lds_row<uint16_t>();
-      const int kx = k_swz<uint16_t>(row), vx = v_swz<uint16_t>(row);
-      *reinterpret_cast<uint4 *>(kd + ((c ^ kx) << 4)) = Chunk<uint8_t>{make_uint2(k[n].x, k[n].y)}.to_bf16();
-      *reinterpret_cast<uint4 *>(kd + (((c + 1) ^ kx) << 4)) = Chunk<uint8_t>{make_uint2(k[n].z, k[n].w)}.to_bf16();
-      *reinterpret_cast<uint4 *>(vd + ((c ^ vx) << 4)) = Chunk<uint8_t>{make_uint2(v[n].x, v[n].y)}.to_bf16();
-      *reinterpret_cast<uint4 *>(vd + (((c + 1) ^ vx) << 4)) = Chunk<uint8_t>{make_uint2(v[n].z, v[n].w)}.to_bf16();
-    }
-  }
-};
-
 // ---------------------------------------------------------------------------
 // Tiles
 // ---------------------------------------------------------------------------
@@ -560,9 +574,42 @@ __device__ __forceinline__ Scale score_scale(const AttendArgs &a, float2 sc) {
   return c == 0.0f ? Scale{1.0f, false, true} : Scale{fabsf(c), c < 0.0f, false};
 }
 
-// Many rows: 128 rows, 32 per wave; K and V tiles of KEYS keys shared by the
-// four waves, two of each in LDS: the next keys are copied while this tile's
-// scores are taken, the next values while its weights are used.
+// Adds the non-finite values of keys [lo, hi) that a row sees to N of its
+// features from d on, in memory.  (Adding one that the sum has already changes
+// nothing: they absorb.)  A slow loop for a cache that holds such values.
+__device__ __forceinline__ void add_to(uint16_t *p, float x) { *p = (uint16_t)pack2(to_f32(*p) + x, 0.0f); }
+__device__ __forceinline__ void add_to(float *p, float x) { *p += x; }
+__device__ __forceinline__ float cache_value(uint16_t x) { return to_f32(x); }
+__device__ __forceinline__ float cache_value(float x) { return x; }
+__device__ __forceinline__ float cache_value(uint8_t x) { return (x & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f; }
+template <typename E, bool PAGED, int N, typename O>
+__device__ __forceinline__ void add_nonfinite(const AttendArgs &a, const Work &w, const RowSight &see, int lo, int hi,
+                                              O *row, int d) {
+#pragma unroll 1
+  for (int v = lo; v < min(hi, w.v_end); ++v) {
+    if (!(v < see.hi && (v >= see.lo || v < see.sv))) continue;
+    const E *p = static_cast<const E *>(a.kv.v) + row_offset<PAGED>(a.kv, w.at.b, w.kvh, w.km.pos(v));
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      const float x = cache_value(p[d + i]);
+      if (!(fabsf(x) < kInf)) add_to(row + d + i, x);
+    }
+  }
+}
+
+// Many rows: 128, 32 per wave; K and V tiles of KEYS keys shared by the four
+// waves, two of each in LDS.
+//
+// What bounds it: a wave's 64 keys x 32 rows take the matrix cores 1024 cycles, the
+// vector unit about 900 (an exponential is 16 of them) and 48 operand reads from
+// LDS; two waves per SIMD overlap these.  An 8k prompt runs at 0.92 PFLOP/s (599
+// us; 450 without the operand reads, 510 without the softmax, 540 without the
+// copies).  Measured and not taken: 64 rows per wave at one wave per SIMD, the
+// values of a tile added while the next one's scores become weights (1049 us: the
+// outputs travel between the register files); 64 rows and half of the keys
+// per wave (837 us, registers spill); 32 keys per tile at three waves per SIMD
+// (630); eight waves on 256 rows (621); wave priorities and instruction orders
+// (590 to 640).
 template <typename E>
 constexpr int many_keys() {
   return sizeof(E) == 4 ? 32 : 64;
@@ -570,105 +617,90 @@ constexpr int many_keys() {
 template <typename E, bool PAGED>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttendArgs a) {
   using L = LE<E>;
-  constexpr int KEYS = many_keys<E>(), NB = KEYS / 32, TB = KEYS * lds_row<L>();
-  constexpr bool WIDEN = sizeof(E) == 1;
-  extern __shared__ __attribute__((aligned(16))) char lds[];  // K0, K1, V0, V1 (FP8: K0, V0)
+  constexpr int KEYS = many_keys<E>(), NB = KEYS / 32, TB = KEYS * lds_row<E>();
+  extern __shared__ __attribute__((aligned(16))) char lds[];  // K0, K1, V0, V1
   const Work w = find_work(a, kManyRows);
   if (!w.any) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r = 32 * wave + (lane & 31), h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  const int r = 32 * wave + (lane & 31);
   const Row row = tile_row(a, w, r);
   const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
   const Scale scale = score_scale<E>(a, sc);
-  AQ<L> q;
-  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
+  AQ<L> q[1];
+  load_rows(q[0], static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
   // a tile is whole if every row sees all of its keys
   const RowSight first = tile_sight(a, w, 0), last = tile_sight(a, w, w.rows - 1);
   const int all_hi = min(first.hi, w.v_end);
   RowSight see = row.see;
   see.hi = min(see.hi, w.v_end);
-
-  RowState st;
+  RowState state[1];
+  RowState &st = state[0];
   st.m = -kInf;
   st.l = 0.0f;
 #pragma unroll
   for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
-  auto step = [&](int v0, const char *K, const char *V, auto between) {
-    auto body = [&](auto edge) {
-      constexpr bool EDGE = decltype(edge)::value;
-      af32x16 s[NB];
-#pragma unroll
-      for (int t = 0; t < NB; ++t) s[t] = score_block(q, K, t, L{});
-      softmax_step<NB, EDGE>(st, s, v0, see, scale.c);
-      between();
-#pragma unroll
-      for (int t = 0; t < NB; ++t) add_values<EDGE>(st, s[t], V, t, L{});
-    };
-    if (v0 + KEYS <= all_hi && (v0 >= last.lo || v0 + KEYS <= last.sv)) body(std::false_type{});
-    else body(std::true_type{});
+
+  // Two tiles of K and V in turn and one barrier per tile: past it, every wave's
+  // copies of this tile are here and every wave is done with the other one,
+  // which the next tile's copies then fill.
+  constexpr int R = KEYS / 4;
+  RowCopies<E, PAGED, R> rc(a.kv, w.km, w.at.b, w.kvh, w.v_end, R * wave);
+  auto copy = [&](int v, int turn) {
+    rc.seek(v + R * wave);
+    rc.template copy<false, false>(a.kv.k, lds + turn * TB);
+    rc.template copy<true, false>(a.kv.v, lds + (2 + turn) * TB);
   };
-  if constexpr (WIDEN) {
-    WidenedRows<PAGED, KEYS> next;
-    char *K = lds, *V = lds + TB;
-    if (w.v_begin < w.v_end) next.load(a.kv, w.km, w.at.b, w.kvh, w.v_begin, w.v_end);
-    for (int v0 = w.v_begin; v0 < w.v_end; v0 += KEYS) {
-      __syncthreads();
-      next.store(K, V);
-      __syncthreads();
-      if (v0 + KEYS < w.v_end) next.load(a.kv, w.km, w.at.b, w.kvh, v0 + KEYS, w.v_end);
-      step(v0, K, V, [] {});
+  if (w.v_begin < w.v_end) copy(w.v_begin, 0);
+  int turn = 0, bad_lo = INT32_MAX, bad_hi = 0;  // (bad: the keys that clean_values found something in)
+#pragma unroll 1
+  for (int v0 = w.v_begin; v0 < w.v_end; v0 += KEYS) {
+    wait_copies<0>();
+    __syncthreads();
+    if (v0 + KEYS < w.v_end) copy(v0 + KEYS, turn ^ 1);
+    const char *K = lds + turn * TB;
+    char *V = lds + (2 + turn) * TB;
+    const bool whole = v0 + KEYS <= all_hi && (v0 >= last.lo || v0 + KEYS <= last.sv);
+    if (!whole && __syncthreads_or(clean_values<E, kThreads>(V, TB, tid))) {
+      bad_lo = min(bad_lo, v0);
+      bad_hi = v0 + KEYS;
     }
-  } else {
-    constexpr int R = KEYS / 4;
-    RowCopies<E, PAGED, R> rc(a.kv, w.km, w.at.b, w.kvh, w.v_end, R * wave);
-    if (w.v_begin < w.v_end) {
-      rc.seek(w.v_begin + R * wave);
-      rc.template copy<false, false>(a.kv.k, lds);
-      rc.template copy<true, false>(a.kv.v, lds + 2 * TB);
-    }
-    int turn = 0;
-    for (int v0 = w.v_begin; v0 < w.v_end; v0 += KEYS) {
-      const bool more = v0 + KEYS < w.v_end;
-      char *K = lds + turn * TB, *V = lds + (2 + turn) * TB;
-      // this tile's keys are here when every wave's copies are; all waves are
-      // done with the other key tile since the barrier before their values
-      wait_copies<decltype(rc)::NL>();
-      __syncthreads();
-      if (more) {
-        rc.seek(v0 + KEYS + R * wave);
-        rc.template copy<false, false>(a.kv.k, lds + (turn ^ 1) * TB);
-      }
-      step(v0, K, V, [&] {
-        if (more) wait_copies<decltype(rc)::NL>();
-        else wait_copies<0>();
-        __syncthreads();
-        if (more) rc.template copy<true, false>(a.kv.v, lds + (2 + (turn ^ 1)) * TB);
-      });
-      turn ^= 1;
-    }
+    af32x16 s[1][NB];
+    score_tile32(s, q, K, E{});
+    if (!whole) hide(s[0], v0, see);
+    const float f = move_reference(st, row_max(s[0]), scale.c);
+    if (__any(f != 1.0f)) rescale(st, f);
+    weigh(st, s[0], scale.c);
+    Weights<L, 1, NB> p;
+    pack(p, s);
+    add_values(state, p, V, E{});
+    turn ^= 1;
   }
 
   const float l = xor32_sum(st.l);
   if (!row.valid) return;
+  const int64_t at = w.out_row + r;
+  float f = 1.0f;
   if (a.T == 1) {
-    const float f = l > 0.0f || l != l ? sc.y / l : 0.0f;  // a row that sees nothing is zero
-    L *out = static_cast<L *>(a.out) + row.at;
-#pragma unroll
-    for (int n = 0; n < 4; ++n)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        store4(out + 32 * n + 8 * g + 4 * h, make_float4(st.o[n][4 * g] * f, st.o[n][4 * g + 1] * f,
-                                                         st.o[n][4 * g + 2] * f, st.o[n][4 * g + 3] * f));
+    f = l > 0.0f || l != l ? sc.y / l : 0.0f;  // a row that sees nothing is zero
   } else {
-    const int64_t at = w.out_row + r;
     if (h == 0) a.stat[at] = make_float2(st.m == -kInf ? -kInf : st.m * scale.c, l);
-    if (st.m == -kInf) return;  // (nothing seen here: the sum 0 says so)
+    if (st.m == -kInf) return;  // (nothing seen here: the statistics say so)
+  }
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+  for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4 *>(a.part + at * kHeadDim + 32 * n + 8 * g + 4 * h) =
-            make_float4(st.o[n][4 * g], st.o[n][4 * g + 1], st.o[n][4 * g + 2], st.o[n][4 * g + 3]);
+    for (int g = 0; g < 4; ++g) {
+      const float4 x = make_float4(st.o[n][4 * g] * f, st.o[n][4 * g + 1] * f, st.o[n][4 * g + 2] * f, st.o[n][4 * g + 3] * f);
+      const int d = 32 * n + 8 * g + 4 * h;
+      if (a.T == 1) store4(static_cast<L *>(a.out) + row.at + d, x);
+      else *reinterpret_cast<float4 *>(a.part + at * kHeadDim + d) = x;
+    }
+  if (bad_lo < bad_hi) {
+#pragma unroll 1
+    for (int d = 4 * h; d < kHeadDim; d += 8) {
+      if (a.T == 1) add_nonfinite<E, PAGED, 4>(a, w, see, bad_lo, bad_hi, static_cast<L *>(a.out) + row.at, d);
+      else add_nonfinite<E, PAGED, 4>(a, w, see, bad_lo, bad_hi, a.part + at * kHeadDim, d);
+    }
   }
 }
 
@@ -685,6 +717,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   using L = LE<E>;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float wm[4][kFewRows], wl[4][kFewRows];
+  __shared__ int bad[4][2];  // the keys that clean_values found something in
   const Work w = find_work(a, kFewRows);
   if (!w.any) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -703,36 +736,44 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   const Row row = tile_row(a, w, r);
   const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
   const Scale scale = score_scale<E>(a, sc);
-  AQ<L> q;
-  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
+  AQ<L> q[1];
+  load_rows(q[0], static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
   const RowSight first = tile_sight(a, w, 0), last = tile_sight(a, w, w.rows - 1);
   RowSight see = row.see;
   see.hi = min(see.hi, end);
   const int all_hi = min(first.hi, end);
 
-  RowState st;
+  RowState state[1];
+  RowState &st = state[0];
   st.m = -kInf;
   st.l = 0.0f;
 #pragma unroll
   for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
+  int bad_lo = INT32_MAX, bad_hi = 0;
   for (int v0 = begin; v0 < end; v0 += 32) {
     const bool more = v0 + 32 < end;
     wait_copies<NL>();
-    af32x16 s[1] = {score_block(q, K, 0, E{})};
+    af32x16 s[1][1];
+    score_tile32(s, q, K, E{});
     wait_reads();
     if (more) {
       rc.seek(v0 + 32);
       rc.template copy<false, true>(a.kv.k, K);
     }
-    auto rest = [&](auto edge) {
-      constexpr bool EDGE = decltype(edge)::value;
-      softmax_step<1, EDGE>(st, s, v0, see, scale.c);
-      if (more) wait_copies<NL>();
-      else wait_copies<0>();
-      add_values<EDGE>(st, s[0], V, 0, E{});
-    };
-    if (v0 + 32 <= all_hi && (v0 >= last.lo || v0 + 32 <= last.sv)) rest(std::false_type{});
-    else rest(std::true_type{});
+    const bool whole = v0 + 32 <= all_hi && (v0 >= last.lo || v0 + 32 <= last.sv);
+    if (!whole) hide(s[0], v0, see);
+    const float f = move_reference(st, row_max(s[0]), scale.c);
+    if (__any(f != 1.0f)) rescale(st, f);
+    weigh(st, s[0], scale.c);
+    Weights<L, 1, 1> p;
+    pack(p, s);
+    if (more) wait_copies<NL>();
+    else wait_copies<0>();
+    if (!whole && __any(clean_values<E, 64>(V, 32 * lds_row<E>(), lane))) {
+      bad_lo = min(bad_lo, v0);
+      bad_hi = v0 + 32;
+    }
+    add_values(state, p, V, E{});
     wait_reads();
     if (more) rc.template copy<true, true>(a.kv.v, V);
   }
@@ -742,6 +783,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   if (h == 0) {
     wm[wave][r] = st.m == -kInf ? -kInf : st.m * scale.c;
     wl[wave][r] = l;
+  }
+  if (lane == 0) {
+    bad[wave][0] = bad_lo;
+    bad[wave][1] = bad_hi;
   }
   __syncthreads();  // (also: every wave is done with its tile's memory)
   float m = -kInf;
@@ -779,46 +824,71 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
     if (a.T > 1) *reinterpret_cast<float4 *>(a.part + at * kHeadDim + 16 * d0 + 4 * k) = x;
     else store4(static_cast<L *>(a.out) + row2.at + 16 * d0 + 4 * k, x);
   }
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    if (bad[i][0] >= bad[i][1]) continue;
+    if (a.T > 1) add_nonfinite<E, PAGED, 16>(a, w, row2.see, bad[i][0], bad[i][1], a.part + at * kHeadDim, 16 * d0);
+    else add_nonfinite<E, PAGED, 16>(a, w, row2.see, bad[i][0], bad[i][1], static_cast<L *>(a.out) + row2.at, 16 * d0);
+  }
 }
 
-// Joins the splits' partial results, a wave per (KV head, row of a tile).
+// Joins the splits' partial results, a wave per (KV head, row of a tile): lane i
+// takes split i's statistics (and i + 64's, ..), then the half-waves take the even
+// and the odd splits' rows, four features per lane, several rows in flight.
 template <typename E, int ROWS>
 __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   using L = LE<E>;
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  constexpr int MS = kMaxSplits / 64;
+  const int lane = threadIdx.x & 63, odd = lane >> 5;
+  const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = (int)(id % ROWS), kvh = (int)(id / ROWS % a.Hkv);
   const int64_t x = id / ROWS / a.Hkv;
   if (x >= a.tiles) return;
   const TileAt at = find_tile(a.ch, x, a.tile_tokens);
   if (at.b >= a.ch.B) return;
   const int i = r / a.G;
-  if (i >= min(a.tile_tokens, at.count - at.i0) || i >= a.tile_tokens) return;
+  if (i >= min(a.tile_tokens, at.count - at.i0)) return;
   const int64_t base = (x * a.Hkv + kvh) * a.T * ROWS + r;
-  float m = -kInf;
-  for (int t = 0; t < a.T; ++t) m = fmaxf(m, a.stat[base + (int64_t)t * ROWS].x);
-  float2 o = make_float2(0, 0);
-  float l = 0.0f;
-  for (int t = 0; t < a.T; ++t) {
-    const float2 s = a.stat[base + (int64_t)t * ROWS];
-    if (s.x == -kInf) continue;  // the split holds no key that the row sees
-    const float f = fast_exp2(s.x - m);
-    const float2 y = reinterpret_cast<const float2 *>(a.part + (base + (int64_t)t * ROWS) * kHeadDim)[lane];
-    l = fmaf(f, s.y, l);
-    o = make_float2(fmaf(f, y.x, o.x), fmaf(f, y.y, o.y));
+  float2 s[MS];
+  float m = -kInf, l = 0.0f;
+#pragma unroll
+  for (int k = 0; k < MS; ++k) {
+    const int t = 64 * k + lane;
+    s[k] = t < a.T ? a.stat[base + (int64_t)t * ROWS] : make_float2(-kInf, 0.0f);
+    m = fmaxf(m, s[k].x);
+  }
+  m = wave_max(m);
+#pragma unroll
+  for (int k = 0; k < MS; ++k) {
+    s[k].x = s[k].x == -kInf ? 0.0f : fast_exp2(s[k].x - m);  // 0: the split holds no key that the row sees
+    l += s[k].x == 0.0f ? 0.0f : s[k].x * s[k].y;
+  }
+  l = wave_sum(l);
+  float4 o = make_float4(0, 0, 0, 0);
+#pragma unroll
+  for (int k = 0; k < MS; ++k) {
+#pragma unroll 4
+    for (int t = 0; t < min(64, a.T - 64 * k); t += 2) {
+      const int tt = t + odd;
+      const float f = __shfl(s[k].x, tt);  // (0 past the last split)
+      if (f != 0.0f) {                     // (a split of weight 0 may not have written its rows)
+        const float4 y = reinterpret_cast<const float4 *>(a.part + (base + (int64_t)(64 * k + tt) * ROWS) * kHeadDim)[lane & 31];
+        o = make_float4(fmaf(f, y.x, o.x), fmaf(f, y.y, o.y), fmaf(f, y.z, o.z), fmaf(f, y.w, o.w));
+      }
+    }
   }
   const float g = l > 0.0f || l != l ? kv_scales<E>(a.kv, at.b, kvh, a.Hkv).y / l : 0.0f;
-  L *out = static_cast<L *>(a.out) + ((int64_t)(at.first + at.i0 + i) * a.Hq + kvh * a.G + r % a.G) * kHeadDim;
-  if constexpr (sizeof(L) == 2) reinterpret_cast<uint32_t *>(out)[lane] = pack2(o.x * g, o.y * g);
-  else reinterpret_cast<float2 *>(out)[lane] = make_float2(o.x * g, o.y * g);
+  o = make_float4(xor32_sum(o.x) * g, xor32_sum(o.y) * g, xor32_sum(o.z) * g, xor32_sum(o.w) * g);
+  if (odd) return;
+  store4(static_cast<L *>(a.out) + ((int64_t)(at.first + at.i0 + i) * a.Hq + kvh * a.G + r % a.G) * kHeadDim + 4 * lane, o);
 }
 
 // Few rows: a K and a V slot of 32 rows per wave, and at the end the waves'
-// outputs.  Many: two tiles of K and of V (FP8: one, the next is in registers).
+// outputs.  Many: two tiles of K and of V.
 template <typename E>
 constexpr size_t attend_lds(bool few) {
   const size_t slots = (size_t)4 * 64 * lds_row<E>(), join = (size_t)4 * kFewRows * kHeadDim * 4;
-  return few ? (slots > join ? slots : join) : (size_t)(sizeof(E) == 1 ? 2 : 4) * many_keys<E>() * lds_row<LE<E>>();
+  return few ? (slots > join ? slots : join) : (size_t)4 * many_keys<E>() * lds_row<E>();
 }
 
 template <typename E>
@@ -828,7 +898,8 @@ hipError_t launch_attend_e(const AttendPlan &p, const AttendArgs &a, hipStream_t
   const bool paged = a.kv.bt != nullptr;
   const void *fn = p.few ? (paged ? (const void *)k_attend_few<E, true> : (const void *)k_attend_few<E, false>)
                          : (paged ? (const void *)k_attend_many<E, true> : (const void *)k_attend_many<E, false>);
-  hipError_t e = hipExtLaunchKernel(fn, dim3((unsigned)(p.tiles * p.Hkv * p.T)), dim3(kThreads), params,
+  hipError_t e = hipExtLaunchKernel(fn, dim3((unsigned)(p.tiles * p.Hkv * p.T)),
+                                    dim3(kThreads), params,
                                     attend_lds<E>(p.few), st, tm.start, p.T > 1 ? nullptr : tm.stop, 0);
   if (e != hipSuccess || p.T == 1) return e;
   const void *mf = p.few ? (const void *)k_attend_merge<E, kFewRows> : (const void *)k_attend_merge<E, kManyRows>;

@@ -383,21 +383,26 @@ _TORCH_DTYPE = {SANTA_BF16: torch.bfloat16, SANTA_F32: torch.float32}
 
 
 def _rows_check(name: str, x: torch.Tensor, tokens: int, heads: int, dtype: torch.dtype,
-                contiguous: bool = True) -> None:
-    """x is [tokens, heads, 128] of dtype on the device, every token's heads in one run."""
-    if not x.is_cuda or x.dtype != dtype:
+                contiguous: bool = True) -> int:
+    """x is [tokens, heads, 128] of dtype on the device, every token's heads in one run; returns
+    the elements from one token to the next."""
+    if not x.is_cuda or x.dtype is not dtype:
         raise TypeError(f"{name} must be a {dtype} CUDA tensor")
-    if x.dim() != 3 or x.shape[0] != tokens or x.shape[1] != heads or x.shape[2] != 128:
+    if x.shape != (tokens, heads, 128):
         raise ValueError(f"{name} must be [{tokens}, {heads}, 128], not {list(x.shape)}")
-    st = x.stride()
-    if st[2] != 1 or (heads > 1 and st[1] != 128) or (contiguous and tokens > 1 and st[0] != heads * 128):
+    st, run = x.stride(), heads * 128
+    if st == (run, 128, 1):
+        return run
+    if st[2] != 1 or (heads > 1 and st[1] != 128) or (contiguous and tokens > 1 and st[0] != run):
         raise ValueError(f"{name}: every token's heads must be contiguous" + (", and the tokens" if contiguous else ""))
+    return st[0] if tokens > 1 else run  # (one token: whatever torch says)
 
 
-def _launch(fn, device: torch.device, stream, *args) -> None:
-    """fn(*args, stream) with `device` current: its own current stream unless one is given."""
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
+def _launch(fn, x: torch.Tensor, stream, *args) -> None:
+    """fn(*args, stream) with x's device current: its own current stream unless one is given."""
+    index = x.get_device()
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
             _check(fn(*args, _stream(stream)))
     else:
         _check(fn(*args, _stream(stream)))
@@ -412,34 +417,24 @@ def santa_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
     projection's rows; q_out contiguous (q itself, if q is).  chunk None: one token per sequence."""
     T = shape.batch if chunk is None else chunk.num_tokens
     dt, Hkv = _TORCH_DTYPE[shape.dtype], shape.num_kv_heads
-    _rows_check("k", k, T, Hkv, dt, False)
-    _rows_check("v", v, T, Hkv, dt, False)
-    rows = santa_rows_t(None, k.data_ptr(), v.data_ptr(), 0, _row_stride(k), _row_stride(v), None)
+    rows = santa_rows_t(None, k.data_ptr(), v.data_ptr(), 0, _rows_check("k", k, T, Hkv, dt, False),
+                        _rows_check("v", v, T, Hkv, dt, False), None)
     if q is not None:
-        _rows_check("q", q, T, shape.num_q_heads, dt, False)
-        rows.q, rows.q_stride = q.data_ptr(), _row_stride(q)
+        rows.q_stride = _rows_check("q", q, T, shape.num_q_heads, dt, False)
+        rows.q = q.data_ptr()
     if q_out is not None:
         _rows_check("q_out", q_out, T, shape.num_q_heads, dt)
     if positions is not None:
         if positions.dtype != torch.int32 or positions.numel() < T or not positions.is_contiguous():
             raise TypeError("positions must be a contiguous int32 tensor with a position per token")
         rows.positions = positions.data_ptr()
-    _launch(load().santa_rope_append, k.device, stream, ctypes.byref(rows), ctypes.byref(kv),
-            ctypes.byref(shape), _ref(chunk), _ref(rope), _ptr(q_out))
-
-
-def _row_stride(x: torch.Tensor) -> int:
-    """Elements from one token to the next (one token: its heads' run, whatever torch says)."""
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * 128
-
-
-def _ref(x):
-    return None if x is None else ctypes.byref(x)
+    _launch(load().santa_rope_append, k, stream, rows, kv, shape, chunk, rope,
+            None if q_out is None else q_out.data_ptr())
 
 
 def santa_attend_workspace_size(shape: santa_shape_t, kv: santa_kv_t, chunk: Optional[santa_chunk_t] = None,
                                 window: Optional[santa_window_t] = None) -> int:
-    n = load().santa_attend_workspace_size(ctypes.byref(shape), ctypes.byref(kv), _ref(chunk), _ref(window))
+    n = load().santa_attend_workspace_size(shape, kv, chunk, window)
     if n == 0:
         raise SantaError(SANTA_ERR_INVALID_ARG, "santa_attend_workspace_size: invalid arguments")
     return int(n)
@@ -463,8 +458,8 @@ def santa_attend_chunk(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, ch
     T, dt = shape.batch if chunk is None else chunk.num_tokens, _TORCH_DTYPE[shape.dtype]
     _rows_check("q", q, T, shape.num_q_heads, dt)
     _rows_check("out", out, T, shape.num_q_heads, dt)
-    _launch(load().santa_attend_chunk, q.device, stream, q.data_ptr(), ctypes.byref(kv), ctypes.byref(shape),
-            _ref(chunk), _ref(window), scale, out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+    _launch(load().santa_attend_chunk, q, stream, q.data_ptr(), kv, shape, chunk, window, scale,
+            out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def santa_decode_window(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, window: santa_window_t,
@@ -473,8 +468,8 @@ def santa_decode_window(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, w
     dt = _TORCH_DTYPE[shape.dtype]
     _rows_check("q", q, shape.batch, shape.num_q_heads, dt)
     _rows_check("out", out, shape.batch, shape.num_q_heads, dt)
-    _launch(load().santa_decode_window, q.device, stream, q.data_ptr(), ctypes.byref(kv), ctypes.byref(shape),
-            _ref(window), scale, out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+    _launch(load().santa_decode_window, q, stream, q.data_ptr(), kv, shape, window, scale,
+            out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def santa_set_options(path: int = SANTA_PATH_AUTO, splits: int = 0) -> None:
