@@ -294,7 +294,7 @@ santa_status_t santa_decode_flash(const void *q, const santa_kv_t *kv, const san
  * graph's size).
  *   q_start:    device int32 [batch + 1], non-decreasing, q_start[0] >= 0; or
  *               NULL: one token per sequence, num_tokens == batch.
- *   num_tokens: rows of the buffers, >= q_start[batch].
+ *   num_tokens: rows of the buffers, >= q_start[batch], at most 2^25.
  *   max_tokens: the most tokens that a sequence is expected to have (host
  *               value; 0 = unknown).  It chooses the kernel, and no result
  *               depends on it. */

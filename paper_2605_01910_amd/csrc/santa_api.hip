@@ -268,6 +268,7 @@ bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15; }
 santa_status_t check_chunk(const santa_chunk_t *ch, const santa_shape_t *sh, santa_chunk_t *out) {
   *out = ch ? *ch : santa_chunk_t{nullptr, sh->batch, 1};
   if (out->num_tokens < 1) return fail(SANTA_ERR_INVALID_ARG, "num_tokens must be >= 1");
+  if (out->num_tokens > (1 << 25)) return fail(SANTA_ERR_UNSUPPORTED, "num_tokens must be at most 2^25");
   if (out->max_tokens < 0) return fail(SANTA_ERR_INVALID_ARG, "max_tokens must be >= 0");
   if (!out->q_start) {
     if (out->num_tokens != sh->batch)
@@ -301,9 +302,20 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
   p.tiles = (ch.num_tokens - n) / p.tile_tokens + n;
   const int64_t keys = win ? std::min<int64_t>(kv->n_k, (int64_t)win->sinks + win->window + p.tile_tokens - 1) : kv->n_k;
   p.step = p.few || p.elem == 1 ? 32 : 64;
-  // about two workgroups per CU, none with fewer keys than its start costs
+  // Splits.  A longer split costs its stream, another split its share of the
+  // joining: the length that balances them grows with the root of the keys (one
+  // token, us at T splits: 1k keys 16.6 at 1, 12.9 at 8, 14.5 at 24; 4k 39 / 15.1
+  // at 12 / 18.5 at 32; 16k 21.8 at 24 / 28.4 at 64).  32-bit full tiles spend
+  // eight times as long on a key and take the root itself (77 tokens over 1k
+  // keys: 147 at 1, 19.5 at 32).  Grids past one workgroup per CU take a whole
+  // second one or none (32k keys: 256 workgroups 32.0, 384 37.6, 512 37.2; two
+  // tiles of them 57.6, 44.4, 40.1).
   const int64_t groups = p.tiles * p.Hkv;
-  int64_t T = std::min<int64_t>(512 / groups, (keys + (p.elem == 1 ? 63 : 127)) / (p.elem == 1 ? 64 : 128));
+  const double root = std::sqrt((double)keys);
+  const bool heavy = p.elem == 1 && !p.few;
+  const int64_t len = std::max<int64_t>(heavy ? 32 : 128, (int64_t)(heavy ? root : 5 * root));
+  int64_t T = keys / len;
+  if (groups * T > 256) T = T >= 512 / groups ? 512 / groups : 256 / groups;
   if (g_opts.splits > 0) T = g_opts.splits;
   p.T = (int)std::max<int64_t>(1, std::min<int64_t>(T, santa::kMaxSplits));
   size_t off = 0;
@@ -378,7 +390,8 @@ santa_status_t attend(const void *q, const santa_kv_t *kv, const santa_shape_t *
   if (misaligned(q) || misaligned(out)) return fail(SANTA_ERR_UNSUPPORTED, "q and out must be 16-byte aligned");
   if (!std::isfinite(scale)) return fail(SANTA_ERR_INVALID_ARG, "scale must be finite");
   const santa::AttendPlan p = make_attend_plan(sh, kv, ch, win);
-  if (p.tiles * p.Hkv * std::max(p.T, p.rows) > INT32_MAX)
+  // a launch counts its threads in 32 bits: 256 per split of a tile, 64 per row that is joined
+  if (p.tiles * p.Hkv * std::max(p.T * santa::kThreads, p.rows * 64) > (int64_t)UINT32_MAX)
     return fail(SANTA_ERR_UNSUPPORTED, "too many tokens times KV heads for one launch");
   s = check_ws(p.total, ws, ws_bytes);
   if (s != SANTA_OK) return s;
@@ -391,7 +404,7 @@ santa_status_t attend(const void *q, const santa_kv_t *kv, const santa_shape_t *
   a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + p.off_part);
   a.Hq = p.Hq;
   a.Hkv = p.Hkv;
-  a.G = p.G;
+  a.g_log2 = ilog2(p.G);
   a.tile_tokens = p.tile_tokens;
   a.T = p.T;
   a.step = p.step;

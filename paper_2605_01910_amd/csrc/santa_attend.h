@@ -522,7 +522,7 @@ __device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile
   w.out_row = ((x * a.Hkv + w.kvh) * a.T + w.t) * rows_per_tile;
   if (!w.any) return w;
   const int L = uniform(seq_len(a.kv, w.at.b)), n = min(a.tile_tokens, w.at.count - w.at.i0);
-  w.rows = n * a.G;
+  w.rows = n << a.g_log2;
   w.p_lo = L - w.at.count + w.at.i0;
   // (a chunk longer than its context: tokens before position 0 see nothing)
   w.km = w.p_lo + n - 1 < 0 ? KeyMap{0, 0, 0, 0, 0} : key_map(max(w.p_lo, 0), w.p_lo + n - 1, a.window, a.sinks);
@@ -533,7 +533,7 @@ __device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile
 }
 
 __device__ __forceinline__ RowSight tile_sight(const AttendArgs &a, const Work &w, int r) {
-  const int p = w.p_lo + r / a.G;
+  const int p = w.p_lo + (r >> a.g_log2);
   return p < 0 ? RowSight{0, 0, 0} : row_sight(w.km, p, a.window);
 }
 
@@ -547,8 +547,8 @@ struct Row {
 __device__ __forceinline__ Row tile_row(const AttendArgs &a, const Work &w, int r) {
   Row x;
   x.valid = r < w.rows;
-  const int rr = min(r, w.rows - 1), i = rr / a.G;
-  x.at = ((int64_t)(w.at.first + w.at.i0 + i) * a.Hq + w.kvh * a.G + rr % a.G) * kHeadDim;
+  const int rr = min(r, w.rows - 1), i = rr >> a.g_log2;
+  x.at = ((int64_t)(w.at.first + w.at.i0 + i) * a.Hq + (w.kvh << a.g_log2) + rr - (i << a.g_log2)) * kHeadDim;
   x.see = tile_sight(a, w, rr);
   return x;
 }
@@ -846,7 +846,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   if (x >= a.tiles) return;
   const TileAt at = find_tile(a.ch, x, a.tile_tokens);
   if (at.b >= a.ch.B) return;
-  const int i = r / a.G;
+  const int i = r >> a.g_log2;
   if (i >= min(a.tile_tokens, at.count - at.i0)) return;
   const int64_t base = (x * a.Hkv + kvh) * a.T * ROWS + r;
   float2 s[MS];
@@ -880,7 +880,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   const float g = l > 0.0f || l != l ? kv_scales<E>(a.kv, at.b, kvh, a.Hkv).y / l : 0.0f;
   o = make_float4(xor32_sum(o.x) * g, xor32_sum(o.y) * g, xor32_sum(o.z) * g, xor32_sum(o.w) * g);
   if (odd) return;
-  store4(static_cast<L *>(a.out) + ((int64_t)(at.first + at.i0 + i) * a.Hq + kvh * a.G + r % a.G) * kHeadDim + 4 * lane, o);
+  store4(static_cast<L *>(a.out) + ((int64_t)(at.first + at.i0 + i) * a.Hq + (kvh << a.g_log2) + r - (i << a.g_log2)) * kHeadDim + 4 * lane, o);
 }
 
 // Few rows: a K and a V slot of 32 rows per wave, and at the end the waves'

@@ -56,7 +56,7 @@ struct AttendArgs {
   void *out;
   float2 *stat;
   float *part;
-  int32_t Hq, Hkv, G, tile_tokens, T, step;
+  int32_t Hq, Hkv, g_log2, tile_tokens, T, step;
   int64_t tiles;
   int32_t window, sinks;  // window 0: every earlier key
   float scale_log2;
