@@ -311,11 +311,13 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
   // second one or none (32k keys: 256 workgroups 32.0, 384 37.6, 512 37.2; two
   // tiles of them 57.6, 44.4, 40.1).
   const int64_t groups = p.tiles * p.Hkv;
+  // (the tiles to expect, where the caller says how long a sequence's chunk may be)
+  const int64_t busy = std::min(p.tiles, n * ((longest + p.tile_tokens - 1) / p.tile_tokens)) * p.Hkv;
   const double root = std::sqrt((double)keys);
   const bool heavy = p.elem == 1 && !p.few;
   const int64_t len = std::max<int64_t>(heavy ? 32 : 128, (int64_t)(heavy ? root : 5 * root));
   int64_t T = keys / len;
-  if (groups * T > 256) T = T >= 512 / groups ? 512 / groups : 256 / groups;
+  if (busy * T > 256) T = T >= 512 / busy ? 512 / busy : 256 / busy;
   if (g_opts.splits > 0) T = g_opts.splits;
   p.T = (int)std::max<int64_t>(1, std::min<int64_t>(T, santa::kMaxSplits));
   size_t off = 0;

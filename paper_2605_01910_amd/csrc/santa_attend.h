@@ -297,18 +297,19 @@ __device__ __forceinline__ bool clean_words(uint4 &w, uint8_t) {  // E4M3: NaN i
   one(w.x), one(w.y), one(w.z), one(w.w);
   return bad;
 }
-// Over `bytes` of V by a team of TEAM lanes; whether there were any.
-template <typename L, int TEAM>
-__device__ __forceinline__ bool clean_values(char *V, int bytes, int tl) {
+// Over BYTES of V by a team of TEAM lanes; whether there were any.
+template <typename L, int BYTES, int TEAM>
+__device__ __forceinline__ bool clean_values(char *V, int tl) {
+  uint4 w[BYTES / 16 / TEAM];
   bool bad = false;
-#pragma unroll 1
-  for (int i = tl * 16; i < bytes; i += TEAM * 16) {
-    uint4 w = *reinterpret_cast<const uint4 *>(V + i);
-    if (clean_words(w, L{})) {
-      *reinterpret_cast<uint4 *>(V + i) = w;
+#pragma unroll
+  for (int i = 0; i < BYTES / 16 / TEAM; ++i) w[i] = *reinterpret_cast<const uint4 *>(V + (i * TEAM + tl) * 16);
+#pragma unroll
+  for (int i = 0; i < BYTES / 16 / TEAM; ++i)
+    if (clean_words(w[i], L{})) {
+      *reinterpret_cast<uint4 *>(V + (i * TEAM + tl) * 16) = w[i];
       bad = true;
     }
-  }
   return bad;
 }
 
@@ -511,10 +512,10 @@ struct Work {
 };
 __device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile) {
   Work w;
-  const int64_t id = blockIdx.x;
-  w.kvh = (int)(id % a.Hkv);
-  w.t = (int)(id / a.Hkv % a.T);
-  const int64_t x = a.tiles - 1 - id / a.Hkv / a.T;
+  const uint32_t id = blockIdx.x, y = id / (uint32_t)a.Hkv, z = y / (uint32_t)a.T;
+  w.kvh = (int)(id - y * a.Hkv);
+  w.t = (int)(y - z * a.T);
+  const int64_t x = a.tiles - 1 - (int64_t)z;
   const TileAt at = find_tile(a.ch, x, a.tile_tokens);
   auto uniform = [](int i) { return __builtin_amdgcn_readfirstlane(i); };
   w.at = TileAt{uniform(at.b), uniform(at.first), uniform(at.count), uniform(at.i0)};
@@ -660,7 +661,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const char *K = lds + turn * TB;
     char *V = lds + (2 + turn) * TB;
     const bool whole = v0 + KEYS <= all_hi && (v0 >= last.lo || v0 + KEYS <= last.sv);
-    if (!whole && __syncthreads_or(clean_values<E, kThreads>(V, TB, tid))) {
+    if (!whole && __syncthreads_or(clean_values<E, TB, kThreads>(V, tid))) {
       bad_lo = min(bad_lo, v0);
       bad_hi = v0 + KEYS;
     }
@@ -769,7 +770,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
     pack(p, s);
     if (more) wait_copies<NL>();
     else wait_copies<0>();
-    if (!whole && __any(clean_values<E, 64>(V, 32 * lds_row<E>(), lane))) {
+    if (!whole && __any(clean_values<E, 32 * lds_row<E>(), 64>(V, lane))) {
       bad_lo = min(bad_lo, v0);
       bad_hi = v0 + 32;
     }
@@ -840,9 +841,11 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   using L = LE<E>;
   constexpr int MS = kMaxSplits / 64;
   const int lane = threadIdx.x & 63, odd = lane >> 5;
-  const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = (int)(id % ROWS), kvh = (int)(id / ROWS % a.Hkv);
-  const int64_t x = id / ROWS / a.Hkv;
+  const uint32_t id = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = (int)(id % ROWS);
+  const uint32_t y = id / ROWS, z = y / (uint32_t)a.Hkv;
+  const int kvh = (int)(y - z * a.Hkv);
+  const int64_t x = z;
   if (x >= a.tiles) return;
   const TileAt at = find_tile(a.ch, x, a.tile_tokens);
   if (at.b >= a.ch.B) return;

@@ -398,14 +398,18 @@ def _rows_check(name: str, x: torch.Tensor, tokens: int, heads: int, dtype: torc
     return st[0] if tokens > 1 else run  # (one token: whatever torch says)
 
 
+# the current stream's handle without a Stream object around it (a microsecond of a call's ten)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
 def _launch(fn, x: torch.Tensor, stream, *args) -> None:
     """fn(*args, stream) with x's device current: its own current stream unless one is given."""
     index = x.get_device()
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
-            _check(fn(*args, _stream(stream)))
+            _check(fn(*args, _raw_stream(index) if stream is None else _stream(stream)))
     else:
-        _check(fn(*args, _stream(stream)))
+        _check(fn(*args, _raw_stream(index) if stream is None else _stream(stream)))
 
 
 def santa_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, kv: santa_kv_t,
