@@ -710,12 +710,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 // keys' and the values' in turn, with no barrier inside the stream, and keeps
 // its own softmax; they join their results through LDS at the end.
 template <typename E>
+constexpr int few_keys() {  // keys per slot: FP8 rows are short, twice as many keep as much in flight
+  return sizeof(E) == 1 ? 64 : 32;
+}
+template <typename E>
 constexpr int few_wgs() {  // workgroups per CU that the slots leave room for
   return sizeof(E) == 4 ? 1 : 2;
 }
 template <typename E, bool PAGED>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wgs<E>()))) void k_attend_few(AttendArgs a) {
   using L = LE<E>;
+  constexpr int KEYS = few_keys<E>(), NB = KEYS / 32, TB = KEYS * lds_row<E>();
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float wm[4][kFewRows], wl[4][kFewRows];
   __shared__ int bad[4][2];  // the keys that clean_values found something in
@@ -723,11 +728,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   if (!w.any) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 31, h = lane >> 5;
-  char *K = lds + wave * 64 * lds_row<E>(), *V = K + 32 * lds_row<E>();
+  char *K = lds + wave * 2 * TB, *V = K + TB;
   // the wave's keys: a quarter of the split's, in whole tiles
-  const int quarter = ((w.v_end - w.v_begin + 3) / 4 + 31) & ~31;
+  const int quarter = ((w.v_end - w.v_begin + 3) / 4 + KEYS - 1) & ~(KEYS - 1);
   const int begin = min(w.v_begin + wave * quarter, w.v_end), end = min(begin + quarter, w.v_end);
-  RowCopies<E, PAGED, 32> rc(a.kv, w.km, w.at.b, w.kvh, end, 0);
+  RowCopies<E, PAGED, KEYS> rc(a.kv, w.km, w.at.b, w.kvh, end, 0);
   constexpr int NL = decltype(rc)::NL;
   if (begin < end) {
     rc.seek(begin);
@@ -751,28 +756,28 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
 #pragma unroll
   for (int n = 0; n < 4; ++n) st.o[n] = af32x16{};
   int bad_lo = INT32_MAX, bad_hi = 0;
-  for (int v0 = begin; v0 < end; v0 += 32) {
-    const bool more = v0 + 32 < end;
+  for (int v0 = begin; v0 < end; v0 += KEYS) {
+    const bool more = v0 + KEYS < end;
     wait_copies<NL>();
-    af32x16 s[1][1];
+    af32x16 s[1][NB];
     score_tile32(s, q, K, E{});
     wait_reads();
     if (more) {
-      rc.seek(v0 + 32);
+      rc.seek(v0 + KEYS);
       rc.template copy<false, true>(a.kv.k, K);
     }
-    const bool whole = v0 + 32 <= all_hi && (v0 >= last.lo || v0 + 32 <= last.sv);
+    const bool whole = v0 + KEYS <= all_hi && (v0 >= last.lo || v0 + KEYS <= last.sv);
     if (!whole) hide(s[0], v0, see);
     const float f = move_reference(st, row_max(s[0]), scale.c);
     if (__any(f != 1.0f)) rescale(st, f);
     weigh(st, s[0], scale.c);
-    Weights<L, 1, 1> p;
+    Weights<L, 1, NB> p;
     pack(p, s);
     if (more) wait_copies<NL>();
     else wait_copies<0>();
-    if (!whole && __any(clean_values<E, 32 * lds_row<E>(), 64>(V, lane))) {
+    if (!whole && __any(clean_values<E, TB, 64>(V, lane))) {
       bad_lo = min(bad_lo, v0);
-      bad_hi = v0 + 32;
+      bad_hi = v0 + KEYS;
     }
     add_values(state, p, V, E{});
     wait_reads();
@@ -795,12 +800,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   for (int i = 0; i < 4; ++i) m = fmaxf(m, wm[i][r]);
   const float f = st.m == -kInf ? 0.0f : fast_exp2(st.m * scale.c - m);
   float4 *part = reinterpret_cast<float4 *>(lds);  // [wave][32 quads of features][32 rows]
+  if (r < w.rows)
 #pragma unroll
-  for (int n = 0; n < 4; ++n)
+    for (int n = 0; n < 4; ++n)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      part[(wave * 32 + 8 * n + 2 * g + h) * 32 + r] = make_float4(st.o[n][4 * g] * f, st.o[n][4 * g + 1] * f,
-                                                                   st.o[n][4 * g + 2] * f, st.o[n][4 * g + 3] * f);
+      for (int g = 0; g < 4; ++g)
+        part[(wave * 32 + 8 * n + 2 * g + h) * 32 + r] = make_float4(st.o[n][4 * g] * f, st.o[n][4 * g + 1] * f,
+                                                                     st.o[n][4 * g + 2] * f, st.o[n][4 * g + 3] * f);
   __syncthreads();
   const int r2 = tid & 31, d0 = tid >> 5;  // row, and its features 16 d0 .. + 15
   if (r2 >= w.rows) return;
@@ -886,11 +892,10 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   store4(static_cast<L *>(a.out) + ((int64_t)(at.first + at.i0 + i) * a.Hq + (kvh << a.g_log2) + r - (i << a.g_log2)) * kHeadDim + 4 * lane, o);
 }
 
-// Few rows: a K and a V slot of 32 rows per wave, and at the end the waves'
-// outputs.  Many: two tiles of K and of V.
+// Few rows: a K and a V slot per wave, and at the end the waves' outputs.  Many: two tiles of K and of V.
 template <typename E>
 constexpr size_t attend_lds(bool few) {
-  const size_t slots = (size_t)4 * 64 * lds_row<E>(), join = (size_t)4 * kFewRows * kHeadDim * 4;
+  const size_t slots = (size_t)4 * 2 * few_keys<E>() * lds_row<E>(), join = (size_t)4 * kFewRows * kHeadDim * 4;
   return few ? (slots > join ? slots : join) : (size_t)4 * many_keys<E>() * lds_row<E>();
 }
 

@@ -21,7 +21,10 @@ CASES = {
     "ragged_paged": dict(lens=RAGGED, layout="paged", pad=5),
     "ragged_paged_1": dict(lens=RAGGED, layout="paged", page=1),
     "ragged_paged_64": dict(lens=RAGGED, layout="paged", page=64),
+    "ragged_paged_8": dict(lens=RAGGED, layout="paged", page=8),
+    "page_past_context": dict(lens=RAGGED, layout="paged", page=2048),
     "padded_rows": dict(lens=RAGGED, gap=8),
+    "padded_pages": dict(lens=RAGGED, layout="paged", gap=8, Hq=5, Hkv=5),
     "group_1": dict(lens=RAGGED, Hq=3, Hkv=3),
     "group_2": dict(lens=RAGGED, Hq=6, Hkv=3, layout="hnd"),
     "group_8": dict(lens=RAGGED, Hq=8, Hkv=1, layout="paged"),
@@ -96,6 +99,41 @@ def test_hidden_values_reach_no_row(kw, value):
         k = bt.rows(bt.k, 0, torch.tensor([63], device=bt.q.device))
         bt.put(bt.k, 0, torch.tensor([63], device=bt.q.device), torch.full_like(k, value))
         assert torch.equal(attend(bt, hint=hint)[:8], clean[:8])
+
+
+@pytest.mark.parametrize("layout", ["nhd", "paged"])
+def test_hidden_fp8_nan(layout):
+    """The NaN code in a value row: in the rows that see it, with and without a window."""
+    for window in (None, (30, 2)):
+        for hint in (0, 1):
+            bt = Batch([(40, 200), (3, 100)], seed=23, fp8=True, layout=layout)
+            at = torch.tensor([170, 185], device=bt.q.device)
+            v = bt.rows(bt.v, 0, at)
+            v[:, :, 5], v[:, :, 9] = 0x7f, 0xff
+            bt.put(bt.v, 0, at, v)
+            check(bt, attend(bt, window, hint=hint), window)
+
+
+def test_nonfinite_values_in_a_split_call():
+    for value in (float("inf"), float("nan")):
+        bt = Batch([(40, 900), (2, 700)], seed=24)
+        at = torch.tensor([880, 899], device=bt.q.device)
+        v = bt.rows(bt.v, 0, at)
+        v[:, :, 100:] = value
+        bt.put(bt.v, 0, at, v)
+        for hint in (0, 1):
+            check(bt, attend(bt, hint=hint, splits=5))
+
+
+def test_a_nan_query_stays_in_its_row():
+    for hint in (0, 1):
+        bt = Batch([(40, 200)], seed=25)
+        clean = attend(bt, hint=hint)
+        bt.q[7, 3, 11] = float("nan")
+        got = attend(bt, hint=hint)
+        assert torch.isnan(got[7, 3]).all()
+        got[7, 3] = clean[7, 3]
+        assert torch.equal(got, clean)
 
 
 def test_window_reads_no_hidden_page():
@@ -209,6 +247,56 @@ def test_workspace_shared_with_the_decode_calls():
         check(bt, dense)
         assert first is None or torch.equal(first, chunk)
         first = chunk
+
+
+def test_streams_and_the_call_timer():
+    """Calls on two streams at once, each with its own workspace; the events of santa_time_next_call
+    span a call's one or two kernels."""
+    bt = Batch([(1, 3000), (200, 900)], seed=26)
+    want = attend(bt)
+    kv, sh, ch = bt.kv(), bt.shape(), bt.chunk()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [S.alloc_attend_workspace(sh, kv, ch) for _ in streams]
+    outs = [torch.zeros_like(bt.q) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, w, o in zip(streams, ws, outs):
+            S.santa_attend_chunk(bt.q, kv, sh, ch, None, SCALE, o, w, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    for splits in (1, 4):
+        with S.options("auto", splits):
+            w = S.alloc_attend_workspace(sh, kv, ch)
+            e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            for x in e:
+                x.record()
+            torch.cuda.synchronize()
+            S.santa_time_next_call(*e)
+            S.santa_attend_chunk(bt.q, kv, sh, ch, None, SCALE, outs[0], w)
+            torch.cuda.synchronize()
+            assert 0 < e[0].elapsed_time(e[1]) < 100
+
+
+def test_without_context_lengths():
+    """No ctx_len: every sequence has n_k keys."""
+    bt = Batch([(5, 300), (0, 300), (40, 300)], seed=27)
+    kv, sh, ch = bt.kv(), bt.shape(), bt.chunk()
+    kv.ctx_len = None
+    out = torch.full_like(bt.q, 7.0)
+    S.santa_attend_chunk(bt.q, kv, sh, ch, None, SCALE, out, S.alloc_attend_workspace(sh, kv, ch))
+    check(bt, out)
+
+
+def test_ends_outside_the_buffers():
+    """q_start entries past num_tokens count as num_tokens, falling ones as none: no call names a
+    row outside its buffers, and the sequences before them are as ever."""
+    bt = Batch([(5, 60), (4, 40), (3, 50)], seed=28)
+    want = attend(bt)
+    bt.q_start[3] = 1000
+    assert torch.equal(attend(bt), want)
+    bt.q_start[:] = torch.tensor([0, 5, 2, 2], dtype=torch.int32)
+    got = attend(bt)
+    assert torch.equal(got[:5], want[:5]) and torch.all(got[5:] == 7.0)
 
 
 def test_argument_checks():
