@@ -709,10 +709,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 // each wave streams its own run of them through its own two slots of LDS, the
 // keys' and the values' in turn, with no barrier inside the stream, and keeps
 // its own softmax; they join their results through LDS at the end.
-template <typename E>
-constexpr int few_keys() {  // keys per slot: FP8 rows are short, twice as many keep as much in flight
-  return sizeof(E) == 1 ? 64 : 32;
-}
+constexpr int kFewKeys = 32;  // keys per slot (FP8, 64 instead: 22.7 us for 20.7 in 16 windows of 2048 keys, level at 32k)
 template <typename E>
 constexpr int few_wgs() {  // workgroups per CU that the slots leave room for
   return sizeof(E) == 4 ? 1 : 2;
@@ -720,7 +717,7 @@ constexpr int few_wgs() {  // workgroups per CU that the slots leave room for
 template <typename E, bool PAGED>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wgs<E>()))) void k_attend_few(AttendArgs a) {
   using L = LE<E>;
-  constexpr int KEYS = few_keys<E>(), NB = KEYS / 32, TB = KEYS * lds_row<E>();
+  constexpr int KEYS = kFewKeys, NB = KEYS / 32, TB = KEYS * lds_row<E>();
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float wm[4][kFewRows], wl[4][kFewRows];
   __shared__ int bad[4][2];  // the keys that clean_values found something in
@@ -876,13 +873,21 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   float4 o = make_float4(0, 0, 0, 0);
 #pragma unroll
   for (int k = 0; k < MS; ++k) {
-#pragma unroll 4
-    for (int t = 0; t < min(64, a.T - 64 * k); t += 2) {
-      const int tt = t + odd;
-      const float f = __shfl(s[k].x, tt);  // (0 past the last split)
-      if (f != 0.0f) {                     // (a split of weight 0 may not have written its rows)
-        const float4 y = reinterpret_cast<const float4 *>(a.part + (base + (int64_t)(64 * k + tt) * ROWS) * kHeadDim)[lane & 31];
-        o = make_float4(fmaf(f, y.x, o.x), fmaf(f, y.y, o.y), fmaf(f, y.z, o.z), fmaf(f, y.w, o.w));
+#pragma unroll 1
+    for (int t = 0; t < min(64, a.T - 64 * k); t += 8) {
+      float f[4];
+      float4 y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int tt = t + 2 * j + odd;
+        f[j] = __shfl(s[k].x, tt);  // (0 past the last split)
+        const int64_t at_row = base + (int64_t)min(64 * k + tt, a.T - 1) * ROWS;
+        y[j] = reinterpret_cast<const float4 *>(a.part + at_row * kHeadDim)[lane & 31];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (f[j] == 0.0f) continue;  // (a split of weight 0 may not have written its rows)
+        o = make_float4(fmaf(f[j], y[j].x, o.x), fmaf(f[j], y[j].y, o.y), fmaf(f[j], y[j].z, o.z), fmaf(f[j], y[j].w, o.w));
       }
     }
   }
@@ -895,7 +900,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
 // Few rows: a K and a V slot per wave, and at the end the waves' outputs.  Many: two tiles of K and of V.
 template <typename E>
 constexpr size_t attend_lds(bool few) {
-  const size_t slots = (size_t)4 * 2 * few_keys<E>() * lds_row<E>(), join = (size_t)4 * kFewRows * kHeadDim * 4;
+  const size_t slots = (size_t)4 * 2 * kFewKeys * lds_row<E>(), join = (size_t)4 * kFewRows * kHeadDim * 4;
   return few ? (slots > join ? slots : join) : (size_t)4 * many_keys<E>() * lds_row<E>();
 }
 
