@@ -603,9 +603,10 @@ __device__ __forceinline__ void add_nonfinite(const AttendArgs &a, const Work &w
 //
 // What bounds it: a wave's 64 keys x 32 rows take the matrix cores 1024 cycles, the
 // vector unit about 900 (an exponential is 16 of them) and 48 operand reads from
-// LDS; two waves per SIMD overlap these.  An 8k prompt runs at 0.92 PFLOP/s (599
-// us; 450 without the operand reads, 510 without the softmax, 540 without the
-// copies).  Measured and not taken: 64 rows per wave at one wave per SIMD, the
+// LDS; two waves per SIMD overlap these in part.  An 8k prompt runs at 1.0 PFLOP/s,
+// 542 us, at the 2.0 GHz that this load holds (left out, the operand reads give 30 %
+// of the time, the softmax 20, the copies 17).
+// Measured beside 600 us and not taken: 64 rows per wave at one wave per SIMD, the
 // values of a tile added while the next one's scores become weights (1049 us: the
 // outputs travel between the register files); 64 rows and half of the keys
 // per wave (837 us, registers spill); 32 keys per tile at three waves per SIMD

@@ -250,8 +250,8 @@ def chunk_of(q_start: Optional[torch.Tensor], num_tokens: int, max_tokens: int =
     """New tokens of a batch: sequence b's are rows q_start[b] .. q_start[b + 1] - 1 (int32
     [batch + 1] on the device; None: one token per sequence).  max_tokens: the most tokens a
     sequence is expected to have (0: unknown)."""
-    if q_start is not None and (q_start.dtype != torch.int32 or not q_start.is_contiguous()):
-        raise TypeError("q_start must be a contiguous int32 tensor")
+    if q_start is not None and (not q_start.is_cuda or q_start.dtype != torch.int32 or not q_start.is_contiguous()):
+        raise TypeError("q_start must be a contiguous int32 CUDA tensor")
     return santa_chunk_t(None if q_start is None else q_start.data_ptr(), int(num_tokens), int(max_tokens))
 
 
@@ -402,9 +402,12 @@ def _rows_check(name: str, x: torch.Tensor, tokens: int, heads: int, dtype: torc
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
-def _launch(fn, x: torch.Tensor, stream, *args) -> None:
-    """fn(*args, stream) with x's device current: its own current stream unless one is given."""
-    index = x.get_device()
+def _launch(fn, tensors, stream, *args) -> None:
+    """fn(*args, stream) with the tensors' device current: its own current stream unless one is given."""
+    index = tensors[0].get_device()
+    for x in tensors:
+        if x.get_device() != index:  # (-1: host memory)
+            raise ValueError("all tensors must be on one device")
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
             _check(fn(*args, _raw_stream(index) if stream is None else _stream(stream)))
@@ -432,7 +435,8 @@ def santa_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
         if positions.dtype != torch.int32 or positions.numel() < T or not positions.is_contiguous():
             raise TypeError("positions must be a contiguous int32 tensor with a position per token")
         rows.positions = positions.data_ptr()
-    _launch(load().santa_rope_append, k, stream, rows, kv, shape, chunk, rope,
+    tensors = [x for x in (k, v, q, q_out, positions) if x is not None]
+    _launch(load().santa_rope_append, tensors, stream, rows, kv, shape, chunk, rope,
             None if q_out is None else q_out.data_ptr())
 
 
@@ -462,7 +466,7 @@ def santa_attend_chunk(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, ch
     T, dt = shape.batch if chunk is None else chunk.num_tokens, _TORCH_DTYPE[shape.dtype]
     _rows_check("q", q, T, shape.num_q_heads, dt)
     _rows_check("out", out, T, shape.num_q_heads, dt)
-    _launch(load().santa_attend_chunk, q, stream, q.data_ptr(), kv, shape, chunk, window, scale,
+    _launch(load().santa_attend_chunk, (q, out, ws), stream, q.data_ptr(), kv, shape, chunk, window, scale,
             out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 
@@ -472,7 +476,7 @@ def santa_decode_window(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, w
     dt = _TORCH_DTYPE[shape.dtype]
     _rows_check("q", q, shape.batch, shape.num_q_heads, dt)
     _rows_check("out", out, shape.batch, shape.num_q_heads, dt)
-    _launch(load().santa_decode_window, q, stream, q.data_ptr(), kv, shape, window, scale,
+    _launch(load().santa_decode_window, (q, out, ws), stream, q.data_ptr(), kv, shape, window, scale,
             out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 

@@ -34,6 +34,10 @@ CASES = {
     "fp8": dict(lens=RAGGED, fp8=True),
     "fp8_paged": dict(lens=RAGGED, fp8=True, layout="paged", Hq=16, Hkv=2, pad=9),
     "fp8_hnd_group_1": dict(lens=RAGGED, fp8=True, layout="hnd", Hq=2, Hkv=2, gap=16),
+    # past one load of 64 table entries, and past the one fetched ahead
+    "long_paged": dict(lens=[(70, 3000), (1, 2500), (9, 1100)], layout="paged"),
+    "long_paged_f32": dict(lens=[(70, 2300)], layout="paged", dtype=F32, Hq=2, Hkv=1),
+    "long_paged_fp8": dict(lens=[(70, 3000), (2, 2500)], layout="paged", fp8=True),
     "many_sequences": dict(lens=[(i % 4, 3 + i) for i in range(150)], layout="paged"),
 }
 WINDOWS = [None, (1, 0), (40, 4), (64, 100), (1000, 1)]
@@ -315,3 +319,40 @@ def test_argument_checks():
         S.santa_attend_chunk(bt.q.transpose(0, 1).contiguous().transpose(0, 1), kv, sh, ch, None, SCALE, out, ws)
     with pytest.raises(S.SantaError):
         S.santa_attend_chunk(bt.q, kv, sh, ch, None, SCALE, out, ws[:256])
+    with pytest.raises(ValueError):
+        S.santa_attend_chunk(bt.q, kv, sh, ch, None, SCALE, out, torch.zeros(ws.numel(), dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        S.chunk_of(bt.q_start.cpu(), bt.T)
+    with pytest.raises(TypeError):
+        S.chunk_of(bt.q_start.long(), bt.T)
+
+
+def test_launch_path_options_are_ignored():
+    """The decode steps' path options change nothing here, FP8 caches included."""
+    for kw in (dict(), dict(fp8=True)):
+        bt = Batch([(40, 90), (1, 300)], seed=29, **kw)
+        want = attend(bt)
+        kv, sh, ch = bt.kv(), bt.shape(), bt.chunk()
+        for path in ("one", "two", "multi", "rows"):
+            with S.options(path):
+                out = torch.full_like(bt.q, 7.0)
+                S.santa_attend_chunk(bt.q, kv, sh, ch, None, SCALE, out, S.alloc_attend_workspace(sh, kv, ch))
+                assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(layout="paged"), dict(fp8=True)], ids=["nhd", "paged", "fp8"])
+def test_shared_prefix_and_equal_rows(kw):
+    """Two sequences over the same cache rows (a batch stride of 0, or the same pages): equal queries
+    give equal outputs, whatever their place in the batch."""
+    bt = Batch([(6, 700), (6, 700)], seed=30, **kw)
+    if bt.layout == "paged":
+        bt.table[1] = bt.table[0]
+    else:
+        bt.k, bt.v = bt.k[:1].expand(2, -1, -1, -1), bt.v[:1].expand(2, -1, -1, -1)
+    if bt.fp8:
+        bt.k_scale[1], bt.v_scale[1] = bt.k_scale[0], bt.v_scale[0]
+    bt.q[6:] = bt.q[:6]
+    for hint in (0, 1):
+        got = attend(bt, (300, 4), hint=hint)
+        assert torch.equal(got[:6], got[6:])
+        check(bt, got, (300, 4))

@@ -297,7 +297,7 @@ def test_argument_checks():
     kv, sh, ch, plan, out = bt.kv(), bt.shape(), bt.chunk(), S.rope_plan(), torch.empty_like(q)
     bad = [dict(q=q.float()), dict(k=k[:1]), dict(v=v[:, :1]), dict(q_out=out.transpose(0, 1)), dict(k=k.cpu()),
            dict(q_out=None), dict(positions=torch.zeros(1, dtype=torch.int32, device="cuda")),
-           dict(positions=torch.zeros(2, device="cuda")), dict(k=k[..., ::2].repeat(1, 1, 2)[..., ::2]), dict(rope=None)]
+           dict(positions=torch.zeros(2, device="cuda")), dict(positions=torch.zeros(2, dtype=torch.int32)), dict(k=k[..., ::2].repeat(1, 1, 2)[..., ::2]), dict(rope=None)]
     for kw in bad:
         args = dict(q=q, k=k, v=v, kv=kv, shape=sh, chunk=ch, rope=plan, q_out=out)
         args.update(kw)
