@@ -327,7 +327,13 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
     return o;
   };
   take(santa::kErrBytes);  // the head that every layout shares (make_plan)
-  take((size_t)santa::kSyncRowsMax * santa::kSyncStride * 4);
+  p.off_sync = take((size_t)santa::kSyncRowsMax * santa::kSyncStride * 4);
+  // With a row per wave to join, the tile's last split does it in passing; more
+  // rows queue up in that one workgroup and are faster in a launch of their own
+  // (us, last split / launch, window of 1024: one sequence of G = 4 11.2 / 12.0, of
+  // G = 8 12.0 / 11.9, 16 of G = 4 17.7 / 18.9, of G = 8 19.8 / 18.9; 32k keys,
+  // G = 4 27.3 / 27.9, G = 8 31.0 / 27.8; two tokens of G = 4 29.2 / 28.2).
+  p.join = p.few && p.T > 1 && p.T <= 64 && longest * p.G <= 4 && groups <= santa::kSyncRowsMax;
   if (p.T > 1) {
     const size_t rows = (size_t)groups * p.T * p.rows;
     p.off_stat = take(rows * 8);
@@ -404,6 +410,7 @@ santa_status_t attend(const void *q, const santa_kv_t *kv, const santa_shape_t *
   a.out = out;
   a.stat = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.off_stat);
   a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + p.off_part);
+  a.sync = p.join ? reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + p.off_sync) : nullptr;
   a.Hq = p.Hq;
   a.Hkv = p.Hkv;
   a.g_log2 = ilog2(p.G);

@@ -507,7 +507,8 @@ struct Work {
   int kvh, t, rows, p_lo;  // rows: valid ones; p_lo: position of the tile's first token
   int v_begin, v_end;
   KeyMap km;
-  int64_t out_row;         // first row of the tile's partial results
+  int64_t group;           // number of the tile and KV head
+  int64_t out_row;         // first row of the split's partial results
   bool any;                // the tile exists
 };
 __device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile) {
@@ -520,7 +521,8 @@ __device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile
   auto uniform = [](int i) { return __builtin_amdgcn_readfirstlane(i); };
   w.at = TileAt{uniform(at.b), uniform(at.first), uniform(at.count), uniform(at.i0)};
   w.any = w.at.b < a.ch.B;
-  w.out_row = ((x * a.Hkv + w.kvh) * a.T + w.t) * rows_per_tile;
+  w.group = x * a.Hkv + w.kvh;
+  w.out_row = (w.group * a.T + w.t) * rows_per_tile;
   if (!w.any) return w;
   const int L = uniform(seq_len(a.kv, w.at.b)), n = min(a.tile_tokens, w.at.count - w.at.i0);
   w.rows = n << a.g_log2;
@@ -576,24 +578,24 @@ __device__ __forceinline__ Scale score_scale(const AttendArgs &a, float2 sc) {
 }
 
 // Adds the non-finite values of keys [lo, hi) that a row sees to N of its
-// features from d on, in memory.  (Adding one that the sum has already changes
+// features from d on: add(i, value).  (Adding one that the sum has already changes
 // nothing: they absorb.)  A slow loop for a cache that holds such values.
 __device__ __forceinline__ void add_to(uint16_t *p, float x) { *p = (uint16_t)pack2(to_f32(*p) + x, 0.0f); }
 __device__ __forceinline__ void add_to(float *p, float x) { *p += x; }
 __device__ __forceinline__ float cache_value(uint16_t x) { return to_f32(x); }
 __device__ __forceinline__ float cache_value(float x) { return x; }
 __device__ __forceinline__ float cache_value(uint8_t x) { return (x & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f; }
-template <typename E, bool PAGED, int N, typename O>
+template <typename E, bool PAGED, int N, typename F>
 __device__ __forceinline__ void add_nonfinite(const AttendArgs &a, const Work &w, const RowSight &see, int lo, int hi,
-                                              O *row, int d) {
+                                              int d, F &&add) {
 #pragma unroll 1
   for (int v = lo; v < min(hi, w.v_end); ++v) {
     if (!(v < see.hi && (v >= see.lo || v < see.sv))) continue;
-    const E *p = static_cast<const E *>(a.kv.v) + row_offset<PAGED>(a.kv, w.at.b, w.kvh, w.km.pos(v));
-#pragma unroll 1
+    const E *p = static_cast<const E *>(a.kv.v) + row_offset<PAGED>(a.kv, w.at.b, w.kvh, w.km.pos(v)) + d;
+#pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float x = cache_value(p[d + i]);
-      if (!(fabsf(x) < kInf)) add_to(row + d + i, x);
+      const float x = cache_value(p[i]);
+      if (!(fabsf(x) < kInf)) add(i, x);
     }
   }
 }
@@ -700,8 +702,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   if (bad_lo < bad_hi) {
 #pragma unroll 1
     for (int d = 4 * h; d < kHeadDim; d += 8) {
-      if (a.T == 1) add_nonfinite<E, PAGED, 4>(a, w, see, bad_lo, bad_hi, static_cast<L *>(a.out) + row.at, d);
-      else add_nonfinite<E, PAGED, 4>(a, w, see, bad_lo, bad_hi, a.part + at * kHeadDim, d);
+      L *out = static_cast<L *>(a.out) + row.at + d;
+      float *part = a.part + at * kHeadDim + d;
+      add_nonfinite<E, PAGED, 4>(a, w, see, bad_lo, bad_hi, d, [&](int i, float x) {
+        if (a.T == 1) add_to(out + i, x);
+        else add_to(part + i, x);
+      });
     }
   }
 }
@@ -722,6 +728,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float wm[4][kFewRows], wl[4][kFewRows];
   __shared__ int bad[4][2];  // the keys that clean_values found something in
+  __shared__ int rank;
   const Work w = find_work(a, kFewRows);
   if (!w.any) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -807,33 +814,84 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
                                                                      st.o[n][4 * g + 2] * f, st.o[n][4 * g + 3] * f);
   __syncthreads();
   const int r2 = tid & 31, d0 = tid >> 5;  // row, and its features 16 d0 .. + 15
-  if (r2 >= w.rows) return;
-  float mm = -kInf, ll = 0.0f;
+  if (r2 < w.rows) {
+    float mm = -kInf, ll = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) mm = fmaxf(mm, wm[i][r2]);
+    for (int i = 0; i < 4; ++i) mm = fmaxf(mm, wm[i][r2]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) ll += wm[i][r2] == -kInf ? 0.0f : fast_exp2(wm[i][r2] - mm) * wl[i][r2];
-  const int64_t at = w.out_row + r2;
-  const float g = a.T > 1 ? 1.0f : ll > 0.0f || ll != ll ? sc.y / ll : 0.0f;
-  const Row row2 = tile_row(a, w, r2);
-  if (a.T > 1 && d0 == 0) a.stat[at] = make_float2(mm, ll);
+    for (int i = 0; i < 4; ++i) ll += wm[i][r2] == -kInf ? 0.0f : fast_exp2(wm[i][r2] - mm) * wl[i][r2];
+    const float g = a.T > 1 ? 1.0f : ll > 0.0f || ll != ll ? sc.y / ll : 0.0f;
+    float x[16];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    float4 x = make_float4(0, 0, 0, 0);
+    for (int k = 0; k < 4; ++k) {
+      float4 s = make_float4(0, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 y = part[(i * 32 + 4 * d0 + k) * 32 + r2];
-      x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+      for (int i = 0; i < 4; ++i) {
+        const float4 y = part[(i * 32 + 4 * d0 + k) * 32 + r2];
+        s = make_float4(s.x + y.x, s.y + y.y, s.z + y.z, s.w + y.w);
+      }
+      x[4 * k] = s.x * g, x[4 * k + 1] = s.y * g, x[4 * k + 2] = s.z * g, x[4 * k + 3] = s.w * g;
     }
-    x = make_float4(x.x * g, x.y * g, x.z * g, x.w * g);
-    if (a.T > 1) *reinterpret_cast<float4 *>(a.part + at * kHeadDim + 16 * d0 + 4 * k) = x;
-    else store4(static_cast<L *>(a.out) + row2.at + 16 * d0 + 4 * k, x);
-  }
+    const Row row2 = tile_row(a, w, r2);
 #pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
-    if (bad[i][0] >= bad[i][1]) continue;
-    if (a.T > 1) add_nonfinite<E, PAGED, 16>(a, w, row2.see, bad[i][0], bad[i][1], a.part + at * kHeadDim, 16 * d0);
-    else add_nonfinite<E, PAGED, 16>(a, w, row2.see, bad[i][0], bad[i][1], static_cast<L *>(a.out) + row2.at, 16 * d0);
+    for (int i = 0; i < 4; ++i)
+      if (bad[i][0] < bad[i][1])
+        add_nonfinite<E, PAGED, 16>(a, w, row2.see, bad[i][0], bad[i][1], 16 * d0, [&](int j, float y) { x[j] += y; });
+    const int64_t at = w.out_row + r2;
+    if (a.T == 1) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        store4(static_cast<L *>(a.out) + row2.at + 16 * d0 + 4 * k,
+               make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]));
+    } else if (!a.sync) {
+      if (d0 == 0) a.stat[at] = make_float2(mm, ll);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        *reinterpret_cast<float4 *>(a.part + at * kHeadDim + 16 * d0 + 4 * k) =
+            make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+    } else {
+      if (d0 == 0) st_coherent(a.stat + at, make_float2(mm, ll));
+      float2 *to = reinterpret_cast<float2 *>(a.part + at * kHeadDim + 16 * d0);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) st_coherent(to + k, make_float2(x[2 * k], x[2 * k + 1]));
+    }
+  }
+  if (a.T == 1 || !a.sync) return;
+
+  // The tile's last split joins them all, a wave per row: every split has stored
+  // its part, coherently, before it counts itself; the last one sees T - 1 before
+  // it and leaves the counter at zero.  Nobody waits.
+  unsigned long long *count = a.sync + w.group * (kSyncStride / 2) + kAttendCounter;
+  wait_stores();
+  __syncthreads();
+  if (tid == 0) {
+    rank = (int)__hip_atomic_fetch_add(count, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (rank == a.T - 1) __hip_atomic_store(count, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (rank != a.T - 1) return;
+  for (int r3 = wave; r3 < w.rows; r3 += 4) {
+    const int64_t base = w.out_row - (int64_t)w.t * kFewRows + r3;  // split 0's
+    const float2 s = lane < a.T ? ld_coherent(a.stat + base + (int64_t)lane * kFewRows) : make_float2(-kInf, 0.0f);
+    const float top = wave_max(s.x), u = s.x == -kInf ? 0.0f : fast_exp2(s.x - top);
+    const float total = wave_sum(u == 0.0f ? 0.0f : u * s.y);
+    float2 o = make_float2(0, 0);
+#pragma unroll 1
+    for (int t = 0; t < a.T; t += 8) {
+      float2 y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        y[j] = ld_coherent(reinterpret_cast<const float2 *>(a.part + (base + (int64_t)min(t + j, a.T - 1) * kFewRows) * kHeadDim) + lane);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float uj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u), min(t + j, 63)));  // (0 past the last)
+        if (t + j < a.T && uj != 0.0f) o = make_float2(fmaf(uj, y[j].x, o.x), fmaf(uj, y[j].y, o.y));
+      }
+    }
+    const float g = total > 0.0f || total != total ? sc.y / total : 0.0f;
+    L *out = static_cast<L *>(a.out) + tile_row(a, w, r3).at;
+    if constexpr (sizeof(L) == 2) reinterpret_cast<uint32_t *>(out)[lane] = pack2(o.x * g, o.y * g);
+    else reinterpret_cast<float2 *>(out)[lane] = make_float2(o.x * g, o.y * g);
   }
 }
 
@@ -914,8 +972,8 @@ hipError_t launch_attend_e(const AttendPlan &p, const AttendArgs &a, hipStream_t
                          : (paged ? (const void *)k_attend_many<E, true> : (const void *)k_attend_many<E, false>);
   hipError_t e = hipExtLaunchKernel(fn, dim3((unsigned)(p.tiles * p.Hkv * p.T)),
                                     dim3(kThreads), params,
-                                    attend_lds<E>(p.few), st, tm.start, p.T > 1 ? nullptr : tm.stop, 0);
-  if (e != hipSuccess || p.T == 1) return e;
+                                    attend_lds<E>(p.few), st, tm.start, p.T > 1 && !p.join ? nullptr : tm.stop, 0);
+  if (e != hipSuccess || p.T == 1 || p.join) return e;
   const void *mf = p.few ? (const void *)k_attend_merge<E, kFewRows> : (const void *)k_attend_merge<E, kManyRows>;
   return hipExtLaunchKernel(mf, dim3((unsigned)(p.tiles * p.Hkv * p.rows / (kThreads / 64))), dim3(kThreads), params,
                             0, st, nullptr, tm.stop, 0);

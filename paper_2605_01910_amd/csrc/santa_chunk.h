@@ -44,6 +44,8 @@ struct AttendPlan {
   int64_t tiles;      // upper bound of the batch's tiles per KV head
   int T;              // key splits per tile; 1: no partial results
   int step;           // split lengths are multiples of this
+  int join;           // a tile's last split joins its splits (few rows); 0: a launch of its own
+  size_t off_sync;    // the shared head's counters (Plan::off_sync)
   size_t off_stat;    // float2 [tiles * Hkv * T * rows] (max in log2 units, sum)
   size_t off_part;    // float [tiles * Hkv * T * rows * 128]
   size_t total;
@@ -56,6 +58,7 @@ struct AttendArgs {
   void *out;
   float2 *stat;
   float *part;
+  unsigned long long *sync;  // the row counters, if the last split joins; else null
   int32_t Hq, Hkv, g_log2, tile_tokens, T, step;
   int64_t tiles;
   int32_t window, sinks;  // window 0: every earlier key
@@ -63,6 +66,7 @@ struct AttendArgs {
 };
 
 constexpr int kFewRows = 32;    // rows of a "few" tile: one matrix instruction's columns
+constexpr int kAttendCounter = 2;  // u64 of a row's sync block that counts a tile's splits: zero between calls
 constexpr int kManyRows = 128;  // rows of a full tile: 32 per wave
 
 hipError_t launch_attend(const AttendPlan &p, const AttendArgs &a, hipStream_t st);

@@ -18,8 +18,9 @@ constexpr int kRowTMax = 64;    // largest number of splits per row of the sched
 // may hold large threshold sets in LDS.
 constexpr int kDirectPollMax = 256;
 // Per KV row, the fused paths keep a sync block of kSyncStride ints: the
-// counters in the first 256 bytes, then (at u64 index kMailOffset) the
-// scheduled sampled path's statistics mailbox, one u64 per (head < 8, split <
+// counters in the first 256 bytes (u64 0 and 1 the decode paths', 2 the splits of
+// a chunk attention's tile, zero between calls), then (at u64 index kMailOffset)
+// the scheduled sampled path's statistics mailbox, one u64 per (head < 8, split <
 // kRowTMax), zero whenever no call is running.
 constexpr int kMailOffset = 32;
 constexpr int kSyncStride = 2 * kMailOffset + 2 * 8 * kRowTMax;

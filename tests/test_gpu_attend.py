@@ -303,6 +303,28 @@ def test_ends_outside_the_buffers():
     assert torch.equal(got[:5], want[:5]) and torch.all(got[5:] == 7.0)
 
 
+def test_calls_leave_the_counters_at_zero():
+    """A call whose last split joins the others (one token, few heads) counts them in the workspace's
+    shared head and clears the count: calls of other shapes and kinds find it as they need it."""
+    head = 256 + 4096 * (2 * 32 + 2 * 8 * 64) * 4
+    one, two = Batch([(1, 4000), (1, 900)], seed=31), Batch([(1, 2500)] * 3, Hq=2, Hkv=1, seed=32, layout="paged")
+    n = max(S.santa_attend_workspace_size(x.shape(), x.kv()) for x in (one, two))
+    n = max(n, S.santa_workspace_size(one.shape(), one.kv(), 1, S.SANTA_KIND_DENSE))
+    ws = torch.empty(n + 256, dtype=torch.uint8, device="cuda")
+    ws = ws[(-ws.data_ptr()) % 256:][:n]
+    S.santa_workspace_init(ws)
+    for _ in range(3):
+        for bt, win in ((one, None), (two, S.window_of(600, 4))):
+            out = torch.full_like(bt.q, 7.0)
+            S.santa_attend_chunk(bt.q, bt.kv(), bt.shape(), None, win, SCALE, out, ws)
+            check(bt, out, (600, 4) if win else None)
+            assert not ws[:head].any()
+    S.santa_decode_dense(one.q, one.kv(), one.shape(), SCALE, out := torch.full_like(one.q, 7.0), ws)
+    check(one, out)
+    S.santa_attend_chunk(one.q, one.kv(), one.shape(), None, None, SCALE, out, ws)
+    check(one, out)
+
+
 def test_argument_checks():
     bt = Batch([(2, 40)], seed=20)
     kv, sh, ch = bt.kv(), bt.shape(), bt.chunk()
