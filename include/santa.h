@@ -14,8 +14,9 @@
  *
  * Conventions shared by every entry point
  * ---------------------------------------
- * - Every pointer argument except `stream` and the `shape`/`kv`/`kt` structs is
- *   a DEVICE pointer owned by the caller.  The library never allocates, frees
+ * - Every pointer argument except `stream` and the structs (`shape`, `kv`, `kt`,
+ *   `chunk`, `window`, `rows`, `rope`, `params`) is a DEVICE pointer owned by the
+ *   caller, and so are the pointers inside the structs.  The library never allocates, frees
  *   or synchronises; all kernels are enqueued on `stream` (a hipStream_t,
  *   NULL = the null stream) and the call returns before they finish.
  * - Element type: `shape->dtype` (SANTA_BF16 or SANTA_F32) is the type of q, K,
@@ -296,8 +297,8 @@ santa_status_t santa_decode_flash(const void *q, const santa_kv_t *kv, const san
  *               NULL: one token per sequence, num_tokens == batch.
  *   num_tokens: rows of the buffers, >= q_start[batch], at most 2^25.
  *   max_tokens: the most tokens that a sequence is expected to have (host
- *               value; 0 = unknown).  It chooses the kernel, and no result
- *               depends on it. */
+ *               value; 0 = unknown).  It chooses the kernel and the splits:
+ *               any value gives the same results within rounding. */
 typedef struct {
   const int32_t *q_start;
   int32_t num_tokens;

@@ -123,10 +123,9 @@ __device__ __forceinline__ void load_rows(AQ<float> &q, const float *p, bool val
   }
 }
 
-// Raw scores (before the scale) of the tile's NB blocks of 32 keys with H blocks
-// of 32 rows: a key operand read from LDS once serves all H.
-template <int H, int NB>
-__device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<uint16_t> (&q)[H], const char *K, uint8_t) {
+// Raw scores (before the scale) of the tile's NB blocks of 32 keys.
+template <int NB>
+__device__ __forceinline__ void score_tile(af32x16 (&s)[NB], const AQ<uint16_t> &q, const char *K, uint8_t) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   const char *row = K + r * lds_row<uint8_t>() + 8 * h;
   const int x = (r >> 1) & 7;
@@ -135,14 +134,12 @@ __device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<uint1
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const Chunk<uint8_t> k{*reinterpret_cast<const uint2 *>(row + 32 * t * lds_row<uint8_t>() + ((i ^ x) << 4))};
-      const abf16x8 k16 = __builtin_bit_cast(abf16x8, k.to_bf16());
-#pragma unroll
-      for (int c = 0; c < H; ++c)
-        s[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k16, q[c].f[i], i ? s[c][t] : af32x16{}, 0, 0, 0);
+      s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(abf16x8, k.to_bf16()), q.f[i],
+                                                     i ? s[t] : af32x16{}, 0, 0, 0);
     }
 }
-template <int H, int NB>
-__device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<uint16_t> (&q)[H], const char *K, uint16_t) {
+template <int NB>
+__device__ __forceinline__ void score_tile(af32x16 (&s)[NB], const AQ<uint16_t> &q, const char *K, uint16_t) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   const char *row = K + r * lds_row<uint16_t>();
   const int x = h ^ (r & 15);
@@ -151,13 +148,11 @@ __device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<uint1
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const abf16x8 k = *reinterpret_cast<const abf16x8 *>(row + 32 * t * lds_row<uint16_t>() + (((2 * i) ^ x) << 4));
-#pragma unroll
-      for (int c = 0; c < H; ++c)
-        s[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c].f[i], i ? s[c][t] : af32x16{}, 0, 0, 0);
+      s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q.f[i], i ? s[t] : af32x16{}, 0, 0, 0);
     }
 }
-template <int H, int NB>
-__device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<float> (&q)[H], const char *K, float) {
+template <int NB>
+__device__ __forceinline__ void score_tile(af32x16 (&s)[NB], const AQ<float> &q, const char *K, float) {
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   const char *row = K + r * lds_row<float>();
   const int x = h ^ (r & 15);
@@ -166,14 +161,11 @@ __device__ __forceinline__ void score_tile32(af32x16 (&s)[H][NB], const AQ<float
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float4 k = *reinterpret_cast<const float4 *>(row + 32 * t * lds_row<float>() + (((2 * i) ^ x) << 4));
-#pragma unroll
-      for (int c = 0; c < H; ++c) {
-        af32x16 y = i ? s[c][t] : af32x16{};
-        y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, q[c].f[i].x, y, 0, 0, 0);
-        y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, q[c].f[i].y, y, 0, 0, 0);
-        y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, q[c].f[i].z, y, 0, 0, 0);
-        s[c][t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, q[c].f[i].w, y, 0, 0, 0);
-      }
+      af32x16 y = i ? s[t] : af32x16{};
+      y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, q.f[i].x, y, 0, 0, 0);
+      y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, q.f[i].y, y, 0, 0, 0);
+      y = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, q.f[i].z, y, 0, 0, 0);
+      s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, q.f[i].w, y, 0, 0, 0);
     }
 }
 
@@ -223,29 +215,27 @@ __device__ __forceinline__ uint32_t nonfinite2(uint32_t w) {
   return ((e & 0xffffu) == 0x7f80u ? 0xffffu : 0u) | ((e >> 16) == 0x7f80u ? 0xffff0000u : 0u);
 }
 
-// The weights of H blocks of rows over NB blocks of keys, as operands.
-template <typename L, int H, int NB>
+// The weights over NB blocks of keys, as operands.
+template <typename L, int NB>
 struct Weights {
-  abf16x8 f[H][2 * NB];  // nearest even: half a step is 2^-9 of a weight; the sum of weights keeps 32 bits
+  abf16x8 f[2 * NB];  // nearest even: at most 2^-8 of a weight; the sum of weights keeps 32 bits
 };
-template <int H, int NB>
-struct Weights<float, H, NB> {
-  af32x16 f[H][NB];
+template <int NB>
+struct Weights<float, NB> {
+  af32x16 f[NB];
 };
 
 // O^T += V^T P^T over the tile at V (rows of type L).
-template <typename L, int H, int NB>
-__device__ __forceinline__ void add_values(RowState (&st)[H], const Weights<QE<L>, H, NB> &p, const char *V, L) {
-  const int lane = threadIdx.x & 63, h = lane >> 5;
+template <typename L, int NB>
+__device__ __forceinline__ void add_values(RowState &st, const Weights<QE<L>, NB> &p, const char *V, L) {
+  const int h = (threadIdx.x >> 5) & 1;
   if constexpr (sizeof(L) <= 2) {
 #pragma unroll
     for (int b = 0; b < 2 * NB; ++b)
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         const abf16x8 w = __builtin_bit_cast(abf16x8, value_operand(V, 16 * b + 4 * h, n, L{}));
-#pragma unroll
-        for (int c = 0; c < H; ++c)
-          st[c].o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p.f[c][b], st[c].o[n], 0, 0, 0);
+        st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p.f[b], st.o[n], 0, 0, 0);
       }
   } else {
 #pragma unroll
@@ -253,12 +243,8 @@ __device__ __forceinline__ void add_values(RowState (&st)[H], const Weights<QE<L
 #pragma unroll
       for (int n = 0; n < 4; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float w = value32(V, t, n, i);
-#pragma unroll
-          for (int c = 0; c < H; ++c)
-            st[c].o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, p.f[c][t][i], st[c].o[n], 0, 0, 0);
-        }
+        for (int i = 0; i < 16; ++i)
+          st.o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(value32(V, t, n, i), p.f[t][i], st.o[n], 0, 0, 0);
   }
 }
 
@@ -266,6 +252,7 @@ __device__ __forceinline__ void add_values(RowState (&st)[H], const Weights<QE<L
 // not reach them as 0 * inf.  In a tile that not all rows see whole, zeros take
 // their place in LDS (clean_values), and add_nonfinite gives them at the end to
 // the rows that do see them.
+//
 // Whether words w hold a non-finite element, and the words with those zeroed.
 __device__ __forceinline__ bool clean_words(uint4 &w, uint16_t) {
   const uint4 f = make_uint4(nonfinite2(w.x), nonfinite2(w.y), nonfinite2(w.z), nonfinite2(w.w));
@@ -367,21 +354,17 @@ __device__ __forceinline__ void weigh(RowState &st, af32x16 (&s)[NB], float c) {
     }
   st.l += l[0] + l[1];
 }
-template <int H, int NB>
-__device__ __forceinline__ void pack(Weights<uint16_t, H, NB> &w, const af32x16 (&s)[H][NB]) {
+template <int NB>
+__device__ __forceinline__ void pack(Weights<uint16_t, NB> &w, const af32x16 (&s)[NB]) {
 #pragma unroll
-  for (int c = 0; c < H; ++c)
+  for (int b = 0; b < 2 * NB; ++b)
 #pragma unroll
-    for (int b = 0; b < 2 * NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w.f[c][b][i] = (__bf16)s[c][b / 2][8 * (b & 1) + i];
+    for (int i = 0; i < 8; ++i) w.f[b][i] = (__bf16)s[b / 2][8 * (b & 1) + i];
 }
-template <int H, int NB>
-__device__ __forceinline__ void pack(Weights<float, H, NB> &w, const af32x16 (&s)[H][NB]) {
+template <int NB>
+__device__ __forceinline__ void pack(Weights<float, NB> &w, const af32x16 (&s)[NB]) {
 #pragma unroll
-  for (int c = 0; c < H; ++c)
-#pragma unroll
-    for (int t = 0; t < NB; ++t) w.f[c][t] = s[c][t];
+  for (int t = 0; t < NB; ++t) w.f[t] = s[t];
 }
 
 // ---------------------------------------------------------------------------
@@ -608,7 +591,8 @@ __device__ __forceinline__ void add_nonfinite(const AttendArgs &a, const Work &w
 // LDS; two waves per SIMD overlap these in part.  An 8k prompt runs at 1.0 PFLOP/s,
 // 542 us, at the 2.0 GHz that this load holds (left out, the operand reads give 30 %
 // of the time, the softmax 20, the copies 17).
-// Measured beside 600 us and not taken: 64 rows per wave at one wave per SIMD, the
+//
+// Measured at a time of 600 us and not taken: 64 rows per wave at one wave per SIMD, the
 // values of a tile added while the next one's scores become weights (1049 us: the
 // outputs travel between the register files); 64 rows and half of the keys
 // per wave (837 us, registers spill); 32 keys per tile at three waves per SIMD
@@ -630,15 +614,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const Row row = tile_row(a, w, r);
   const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
   const Scale scale = score_scale<E>(a, sc);
-  AQ<L> q[1];
-  load_rows(q[0], static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
+  AQ<L> q;
+  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
   // a tile is whole if every row sees all of its keys
   const RowSight first = tile_sight(a, w, 0), last = tile_sight(a, w, w.rows - 1);
   const int all_hi = min(first.hi, w.v_end);
   RowSight see = row.see;
   see.hi = min(see.hi, w.v_end);
-  RowState state[1];
-  RowState &st = state[0];
+  RowState st;
   st.m = -kInf;
   st.l = 0.0f;
 #pragma unroll
@@ -668,15 +651,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       bad_lo = min(bad_lo, v0);
       bad_hi = v0 + KEYS;
     }
-    af32x16 s[1][NB];
-    score_tile32(s, q, K, E{});
-    if (!whole) hide(s[0], v0, see);
-    const float f = move_reference(st, row_max(s[0]), scale.c);
+    af32x16 s[NB];
+    score_tile(s, q, K, E{});
+    if (!whole) hide(s, v0, see);
+    const float f = move_reference(st, row_max(s), scale.c);
     if (__any(f != 1.0f)) rescale(st, f);
-    weigh(st, s[0], scale.c);
-    Weights<L, 1, NB> p;
+    weigh(st, s, scale.c);
+    Weights<L, NB> p;
     pack(p, s);
-    add_values(state, p, V, E{});
+    add_values(st, p, V, E{});
     turn ^= 1;
   }
 
@@ -747,15 +730,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   const Row row = tile_row(a, w, r);
   const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
   const Scale scale = score_scale<E>(a, sc);
-  AQ<L> q[1];
-  load_rows(q[0], static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
+  AQ<L> q;
+  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
   const RowSight first = tile_sight(a, w, 0), last = tile_sight(a, w, w.rows - 1);
   RowSight see = row.see;
   see.hi = min(see.hi, end);
   const int all_hi = min(first.hi, end);
 
-  RowState state[1];
-  RowState &st = state[0];
+  RowState st;
   st.m = -kInf;
   st.l = 0.0f;
 #pragma unroll
@@ -764,19 +746,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   for (int v0 = begin; v0 < end; v0 += KEYS) {
     const bool more = v0 + KEYS < end;
     wait_copies<NL>();
-    af32x16 s[1][NB];
-    score_tile32(s, q, K, E{});
+    af32x16 s[NB];
+    score_tile(s, q, K, E{});
     wait_reads();
     if (more) {
       rc.seek(v0 + KEYS);
       rc.template copy<false, true>(a.kv.k, K);
     }
     const bool whole = v0 + KEYS <= all_hi && (v0 >= last.lo || v0 + KEYS <= last.sv);
-    if (!whole) hide(s[0], v0, see);
-    const float f = move_reference(st, row_max(s[0]), scale.c);
+    if (!whole) hide(s, v0, see);
+    const float f = move_reference(st, row_max(s), scale.c);
     if (__any(f != 1.0f)) rescale(st, f);
-    weigh(st, s[0], scale.c);
-    Weights<L, 1, NB> p;
+    weigh(st, s, scale.c);
+    Weights<L, NB> p;
     pack(p, s);
     if (more) wait_copies<NL>();
     else wait_copies<0>();
@@ -784,7 +766,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
       bad_lo = min(bad_lo, v0);
       bad_hi = v0 + KEYS;
     }
-    add_values(state, p, V, E{});
+    add_values(st, p, V, E{});
     wait_reads();
     if (more) rc.template copy<true, true>(a.kv.v, V);
   }
