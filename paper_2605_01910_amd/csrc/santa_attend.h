@@ -484,7 +484,13 @@ __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0
 // ---------------------------------------------------------------------------
 // A workgroup's tile and key range.  Blocks are numbered KV head fastest (with
 // 8 KV heads each XCD works on one head's keys), then split, then tile from
-// the batch's last to its first: in a chunk the later tiles see more keys.
+// the last to the first: in a chunk the later tiles see more keys.  The grid has
+// the tiles to expect; where a batch may have more (MORE: rows enough for chunks
+// longer than max_tokens says), each workgroup goes on with every grid_tiles-th
+// one.  A grid for all that there may be would spend its time on empty workgroups:
+// one token with 2000 padding rows over 2k keys 13.7 us, 91.7 with a workgroup for
+// every tile that the rows could make.  (Without the loop 11.1 us for 12.0 in one
+// user's window.)
 struct Work {
   TileAt at;
   int kvh, t, rows, p_lo;  // rows: valid ones; p_lo: position of the tile's first token
@@ -494,12 +500,14 @@ struct Work {
   int64_t out_row;         // first row of the split's partial results
   bool any;                // the tile exists
 };
-__device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile) {
+__device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile, int turn) {
   Work w;
   const uint32_t id = blockIdx.x, y = id / (uint32_t)a.Hkv, z = y / (uint32_t)a.T;
   w.kvh = (int)(id - y * a.Hkv);
   w.t = (int)(y - z * a.T);
-  const int64_t x = a.tiles - 1 - (int64_t)z;
+  const int64_t x = a.grid_tiles - 1 - (int64_t)z + turn * a.grid_tiles;
+  w.any = x < a.tiles;
+  if (!w.any) return w;
   const TileAt at = find_tile(a.ch, x, a.tile_tokens);
   auto uniform = [](int i) { return __builtin_amdgcn_readfirstlane(i); };
   w.at = TileAt{uniform(at.b), uniform(at.first), uniform(at.count), uniform(at.i0)};
@@ -603,12 +611,9 @@ constexpr int many_keys() {
   return sizeof(E) == 4 ? 32 : 64;
 }
 template <typename E, bool PAGED>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttendArgs a) {
+__device__ __forceinline__ void many_tile(const AttendArgs &a, const Work &w, char *lds) {  // lds: K0, K1, V0, V1
   using L = LE<E>;
   constexpr int KEYS = many_keys<E>(), NB = KEYS / 32, TB = KEYS * lds_row<E>();
-  extern __shared__ __attribute__((aligned(16))) char lds[];  // K0, K1, V0, V1
-  const Work w = find_work(a, kManyRows);
-  if (!w.any) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   const int r = 32 * wave + (lane & 31);
   const Row row = tile_row(a, w, r);
@@ -695,6 +700,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 }
 
+template <typename E, bool PAGED, bool MORE>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttendArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  for (int turn = 0; MORE || turn == 0; ++turn) {
+    const Work w = find_work(a, kManyRows, turn);
+    if (!w.any) return;
+    if (turn) __syncthreads();  // every wave is done with the last tile's memory
+    many_tile<E, PAGED>(a, w, lds);
+  }
+}
+
 // Few rows: up to 32, the same for all four waves, which share out the keys:
 // each wave streams its own run of them through its own two slots of LDS, the
 // keys' and the values' in turn, with no barrier inside the stream, and keeps
@@ -705,15 +721,12 @@ constexpr int few_wgs() {  // workgroups per CU that the slots leave room for
   return sizeof(E) == 4 ? 1 : 2;
 }
 template <typename E, bool PAGED>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wgs<E>()))) void k_attend_few(AttendArgs a) {
+__device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, char *lds) {
   using L = LE<E>;
   constexpr int KEYS = kFewKeys, NB = KEYS / 32, TB = KEYS * lds_row<E>();
-  extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float wm[4][kFewRows], wl[4][kFewRows];
   __shared__ int bad[4][2];  // the keys that clean_values found something in
   __shared__ int rank;
-  const Work w = find_work(a, kFewRows);
-  if (!w.any) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 31, h = lane >> 5;
   char *K = lds + wave * 2 * TB, *V = K + TB;
@@ -877,6 +890,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   }
 }
 
+template <typename E, bool PAGED, bool MORE>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wgs<E>()))) void k_attend_few(AttendArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  for (int turn = 0; MORE || turn == 0; ++turn) {
+    const Work w = find_work(a, kFewRows, turn);
+    if (!w.any) return;
+    if (turn) __syncthreads();  // every wave is done with the last tile's memory
+    few_tile<E, PAGED>(a, w, lds);
+  }
+}
+
 // Joins the splits' partial results, a wave per (KV head, row of a tile): lane i
 // takes split i's statistics (and i + 64's, ..), then the half-waves take the even
 // and the odd splits' rows, four features per lane, several rows in flight.
@@ -889,53 +913,54 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   const int r = (int)(id % ROWS);
   const uint32_t y = id / ROWS, z = y / (uint32_t)a.Hkv;
   const int kvh = (int)(y - z * a.Hkv);
-  const int64_t x = z;
-  if (x >= a.tiles) return;
-  const TileAt at = find_tile(a.ch, x, a.tile_tokens);
-  if (at.b >= a.ch.B) return;
-  const int i = r >> a.g_log2;
-  if (i >= min(a.tile_tokens, at.count - at.i0)) return;
-  const int64_t base = (x * a.Hkv + kvh) * a.T * ROWS + r;
-  float2 s[MS];
-  float m = -kInf, l = 0.0f;
-#pragma unroll
-  for (int k = 0; k < MS; ++k) {
-    const int t = 64 * k + lane;
-    s[k] = t < a.T ? a.stat[base + (int64_t)t * ROWS] : make_float2(-kInf, 0.0f);
-    m = fmaxf(m, s[k].x);
-  }
-  m = wave_max(m);
-#pragma unroll
-  for (int k = 0; k < MS; ++k) {
-    s[k].x = s[k].x == -kInf ? 0.0f : fast_exp2(s[k].x - m);  // 0: the split holds no key that the row sees
-    l += s[k].x == 0.0f ? 0.0f : s[k].x * s[k].y;
-  }
-  l = wave_sum(l);
-  float4 o = make_float4(0, 0, 0, 0);
-#pragma unroll
-  for (int k = 0; k < MS; ++k) {
 #pragma unroll 1
-    for (int t = 0; t < min(64, a.T - 64 * k); t += 8) {
-      float f[4];
-      float4 y[4];
+  for (int64_t x = z; x < a.tiles; x += a.grid_tiles) {
+    const TileAt at = find_tile(a.ch, x, a.tile_tokens);
+    if (at.b >= a.ch.B) return;
+    const int i = r >> a.g_log2;
+    if (i >= min(a.tile_tokens, at.count - at.i0)) continue;
+    const int64_t base = (x * a.Hkv + kvh) * a.T * ROWS + r;
+    float2 s[MS];
+    float m = -kInf, l = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int tt = t + 2 * j + odd;
-        f[j] = __shfl(s[k].x, tt);  // (0 past the last split)
-        const int64_t at_row = base + (int64_t)min(64 * k + tt, a.T - 1) * ROWS;
-        y[j] = reinterpret_cast<const float4 *>(a.part + at_row * kHeadDim)[lane & 31];
-      }
+    for (int k = 0; k < MS; ++k) {
+      const int t = 64 * k + lane;
+      s[k] = t < a.T ? a.stat[base + (int64_t)t * ROWS] : make_float2(-kInf, 0.0f);
+      m = fmaxf(m, s[k].x);
+    }
+    m = wave_max(m);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (f[j] == 0.0f) continue;  // (a split of weight 0 may not have written its rows)
-        o = make_float4(fmaf(f[j], y[j].x, o.x), fmaf(f[j], y[j].y, o.y), fmaf(f[j], y[j].z, o.z), fmaf(f[j], y[j].w, o.w));
+    for (int k = 0; k < MS; ++k) {
+      s[k].x = s[k].x == -kInf ? 0.0f : fast_exp2(s[k].x - m);  // 0: the split holds no key that the row sees
+      l += s[k].x == 0.0f ? 0.0f : s[k].x * s[k].y;
+    }
+    l = wave_sum(l);
+    float4 o = make_float4(0, 0, 0, 0);
+#pragma unroll
+    for (int k = 0; k < MS; ++k) {
+#pragma unroll 1
+      for (int t = 0; t < min(64, a.T - 64 * k); t += 8) {
+        float f[4];
+        float4 y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int tt = t + 2 * j + odd;
+          f[j] = __shfl(s[k].x, tt);  // (0 past the last split)
+          const int64_t at_row = base + (int64_t)min(64 * k + tt, a.T - 1) * ROWS;
+          y[j] = reinterpret_cast<const float4 *>(a.part + at_row * kHeadDim)[lane & 31];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (f[j] == 0.0f) continue;  // (a split of weight 0 may not have written its rows)
+          o = make_float4(fmaf(f[j], y[j].x, o.x), fmaf(f[j], y[j].y, o.y), fmaf(f[j], y[j].z, o.z), fmaf(f[j], y[j].w, o.w));
+        }
       }
     }
+    const float g = l > 0.0f || l != l ? kv_scales<E>(a.kv, at.b, kvh, a.Hkv).y / l : 0.0f;
+    o = make_float4(xor32_sum(o.x) * g, xor32_sum(o.y) * g, xor32_sum(o.z) * g, xor32_sum(o.w) * g);
+    const int64_t row = (int64_t)(at.first + at.i0 + i) * a.Hq + (kvh << a.g_log2) + r - (i << a.g_log2);
+    if (!odd) store4(static_cast<L *>(a.out) + row * kHeadDim + 4 * lane, o);
   }
-  const float g = l > 0.0f || l != l ? kv_scales<E>(a.kv, at.b, kvh, a.Hkv).y / l : 0.0f;
-  o = make_float4(xor32_sum(o.x) * g, xor32_sum(o.y) * g, xor32_sum(o.z) * g, xor32_sum(o.w) * g);
-  if (odd) return;
-  store4(static_cast<L *>(a.out) + ((int64_t)(at.first + at.i0 + i) * a.Hq + (kvh << a.g_log2) + r - (i << a.g_log2)) * kHeadDim + 4 * lane, o);
 }
 
 // Few rows: a K and a V slot per wave, and at the end the waves' outputs.  Many: two tiles of K and of V.
@@ -949,15 +974,20 @@ template <typename E>
 hipError_t launch_attend_e(const AttendPlan &p, const AttendArgs &a, hipStream_t st) {
   const CallTimer tm = call_timer();
   void *params[] = {const_cast<AttendArgs *>(&a)};
-  const bool paged = a.kv.bt != nullptr;
-  const void *fn = p.few ? (paged ? (const void *)k_attend_few<E, true> : (const void *)k_attend_few<E, false>)
-                         : (paged ? (const void *)k_attend_many<E, true> : (const void *)k_attend_many<E, false>);
-  hipError_t e = hipExtLaunchKernel(fn, dim3((unsigned)(p.tiles * p.Hkv * p.T)),
+  const void *fn = nullptr;
+  auto pick = [&](auto paged, auto more) {
+    constexpr bool P = decltype(paged)::value, M = decltype(more)::value;
+    fn = p.few ? (const void *)k_attend_few<E, P, M> : (const void *)k_attend_many<E, P, M>;
+  };
+  const bool more = p.grid_tiles < p.tiles;
+  if (a.kv.bt) more ? pick(std::true_type{}, std::true_type{}) : pick(std::true_type{}, std::false_type{});
+  else more ? pick(std::false_type{}, std::true_type{}) : pick(std::false_type{}, std::false_type{});
+  hipError_t e = hipExtLaunchKernel(fn, dim3((unsigned)(p.grid_tiles * p.Hkv * p.T)),
                                     dim3(kThreads), params,
                                     attend_lds<E>(p.few), st, tm.start, p.T > 1 && !p.join ? nullptr : tm.stop, 0);
   if (e != hipSuccess || p.T == 1 || p.join) return e;
   const void *mf = p.few ? (const void *)k_attend_merge<E, kFewRows> : (const void *)k_attend_merge<E, kManyRows>;
-  return hipExtLaunchKernel(mf, dim3((unsigned)(p.tiles * p.Hkv * p.rows / (kThreads / 64))), dim3(kThreads), params,
+  return hipExtLaunchKernel(mf, dim3((unsigned)(p.grid_tiles * p.Hkv * p.rows / (kThreads / 64))), dim3(kThreads), params,
                             0, st, nullptr, tm.stop, 0);
 }
 

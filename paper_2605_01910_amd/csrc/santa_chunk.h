@@ -42,6 +42,7 @@ struct AttendPlan {
   int rows;           // query rows (tokens x group) per tile
   int tile_tokens;    // tokens per tile: rows / G
   int64_t tiles;      // upper bound of the batch's tiles per KV head
+  int64_t grid_tiles; // tiles to expect: the grid's; a workgroup takes every grid_tiles-th one
   int T;              // key splits per tile; 1: no partial results
   int step;           // split lengths are multiples of this
   int join;           // a tile's last split joins its splits (few rows); 0: a launch of its own
@@ -60,7 +61,7 @@ struct AttendArgs {
   float *part;
   unsigned long long *sync;  // the row counters, if the last split joins; else null
   int32_t Hq, Hkv, g_log2, tile_tokens, T, step;
-  int64_t tiles;
+  int64_t tiles, grid_tiles;
   int32_t window, sinks;  // window 0: every earlier key
   float scale_log2;
 };

@@ -52,6 +52,10 @@ __device__ __forceinline__ float2 turn(int64_t pos, uint64_t step, float gain) {
 
 }  // namespace
 
+// Bound by HBM on prompts (q, k and v read once, their results written once: 16k
+// tokens of 48 heads in 77 us, 5.2 TB/s, a copy's rate), by the launch and the
+// chain of table, length and row loads on single tokens (3.7 us).
+//
 // One workgroup rotates and stores TT tokens.  Wave w finds token w's sequence
 // and cache row and takes the token's 64 angles, one per lane, for all its
 // heads; then all threads pass over the (token, head, unit) items, a unit being
@@ -160,7 +164,10 @@ template <typename Q, typename E>
 static hipError_t launch_rope_e(const RopeArgs &a, hipStream_t st) {
   const CallTimer tm = call_timer();
   void *params[] = {const_cast<RopeArgs *>(&a)};
-  const bool one = a.ch.tokens < 1024;
+  // Four tokens per workgroup pay where one has too few items to fill it, on long
+  // chunks (us, one / four: 10 heads 2048 tokens 4.6 / 5.2, 4096 7.5 / 6.2, 16384
+  // 24.1 / 16.9; 48 heads 1024 6.4 / 8.0, 4096 19.3 / 18.7, 16384 77 / 81).
+  const bool one = a.ch.tokens < 4096 || (a.Hq + 2 * a.Hkv) * (kHeadDim / 16) >= kThreads;
   const void *fn = one ? (const void *)k_rope_append<Q, E, 1> : (const void *)k_rope_append<Q, E, 4>;
   return hipExtLaunchKernel(fn, dim3(one ? a.ch.tokens : (a.ch.tokens + 3) / 4), dim3(kThreads), params, 0, st,
                             tm.start, tm.stop, 0);

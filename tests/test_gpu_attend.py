@@ -46,9 +46,10 @@ WINDOWS = [None, (1, 0), (40, 4), (64, 100), (1000, 1)]
 @pytest.mark.parametrize("window", WINDOWS, ids=str)
 @pytest.mark.parametrize("case", sorted(CASES))
 def test_chunk(case, window):
-    """Both kernels (by the hint), unsplit and split."""
+    """Both kernels (by the hint), unsplit and split; hints that are too small (1 for the few-row
+    kernel, 9 to 33 tokens for full tiles) leave tiles that the grid was not made for."""
     bt = Batch(seed=len(case), **CASES[case])
-    for hint in (0, 1):
+    for hint in (0, 1, 32 // bt.G + 1):
         for splits in (0, 3):
             check(bt, attend(bt, window, hint=hint, splits=splits), window)
 
@@ -187,6 +188,15 @@ def test_offsets_past_32_bits():
     for hint in (0, 1):
         for window in (None, (100, 4)):
             check(bt, attend(bt, window, hint=hint), window)
+
+
+def test_much_padding():
+    """Far more rows than tokens: a batch captured for a larger one."""
+    for kw in (dict(), dict(layout="paged", fp8=True)):
+        bt = Batch([(1, 900), (5, 700), (0, 3), (40, 300)], pad=1500, seed=33, **kw)
+        for hint in (0, 1, 5, 40, 100):
+            for splits in (0, 3):
+                check(bt, attend(bt, (200, 4), hint=hint, splits=splits), (200, 4))
 
 
 def test_the_same_call_twice_is_equal():
