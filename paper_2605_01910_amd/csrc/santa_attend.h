@@ -596,8 +596,8 @@ __device__ __forceinline__ void add_nonfinite(const AttendArgs &a, const Work &w
 //
 // What bounds it: a wave's 64 keys x 32 rows take the matrix cores 1024 cycles, the
 // vector unit about 900 (an exponential is 16 of them) and 48 operand reads from
-// LDS; two waves per SIMD overlap these in part.  An 8k prompt runs at 1.0 PFLOP/s,
-// 542 us, at the 2.0 GHz that this load holds (left out, the operand reads give 30 %
+// LDS; two waves per SIMD overlap these in part.  An 8k prompt runs at 0.98 to 1.0
+// PFLOP/s, 542 to 565 us, at the 2.0 GHz that this load holds (left out, the operand reads give 30 %
 // of the time, the softmax 20, the copies 17).
 //
 // Measured at a time of 600 us and not taken: 64 rows per wave at one wave per SIMD, the
