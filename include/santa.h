@@ -290,11 +290,13 @@ santa_status_t santa_decode_flash(const void *q, const santa_kv_t *kv, const san
  * take the LAST positions of its ctx_len[b] keys (n_k without ctx_len): with c
  * tokens, token i stands at position ctx_len[b] - c + i, so one token stands
  * where the decode calls have the current one.  A sequence may have none.  Rows
- * from q_start[batch] to num_tokens - 1 hold no token: they are not read and
- * their output rows are left as they were (a batch padded to a captured
- * graph's size).
- *   q_start:    device int32 [batch + 1], non-decreasing, q_start[0] >= 0; or
- *               NULL: one token per sequence, num_tokens == batch.
+ * before q_start[0] and from q_start[batch] to num_tokens - 1 hold no token: they
+ * are not read or stored and their output rows are left as they were (a view into
+ * longer prefix sums; a batch padded to a captured graph's size).
+ *   q_start:    device int32 [batch + 1], non-decreasing, q_start[0] >= 0
+ *               (entries past num_tokens count as num_tokens, a sequence whose
+ *               end lies below its start has no tokens); or NULL: one token per
+ *               sequence, num_tokens == batch.
  *   num_tokens: rows of the buffers, >= q_start[batch], at most 2^25.
  *   max_tokens: the most tokens that a sequence is expected to have (host
  *               value; 0 = unknown).  It chooses the kernel and the splits:

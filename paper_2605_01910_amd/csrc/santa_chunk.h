@@ -75,31 +75,41 @@ template <typename E>
 hipError_t launch_attend_e(const AttendPlan &p, const AttendArgs &a, hipStream_t st);
 
 #ifdef __HIPCC__
-// The sequence of token t and the range of its tokens, by the whole wave: 64
-// ends per load, no search chain.  b = B when no sequence holds the token.
+// Sequence i's range of rows.  Ends outside [0, tokens] are clamped and falling
+// ones hold nothing, so no row outside the buffers is ever named.
+struct RowRange {
+  int first, end;
+};
+__device__ __forceinline__ RowRange row_range(const ChunkView &c, int i) {
+  const int s = min(max(c.q_start[i], 0), c.tokens);
+  return RowRange{s, min(max(c.q_start[i + 1], s), c.tokens)};
+}
+
+// The sequence that row t belongs to and the range of its rows, by the whole
+// wave: 64 sequences per load, no search chain.  b = B where none holds it (rows
+// before the first sequence's and behind the last one's).
 struct TokenAt {
   int b, first, count;
 };
 __device__ __forceinline__ TokenAt find_token(const ChunkView &c, int t) {
   if (!c.q_start) return t < c.B ? TokenAt{t, t, 1} : TokenAt{c.B, 0, 0};
   const int lane = threadIdx.x & 63;
-  int b = 0;
   for (int base = 0; base < c.B; base += 64) {
     const int i = base + lane;
-    const bool before = i < c.B && c.q_start[i + 1] <= t;
-    const int n = __popcll(__ballot(before));
-    b = base + n;
-    if (n < 64) break;
+    const RowRange r = i < c.B ? row_range(c, i) : RowRange{0, 0};
+    const unsigned long long hit = __ballot(r.first <= t && t < r.end);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int first = __shfl(r.first, l), end = __shfl(r.end, l);
+      return TokenAt{base + l, first, end - first};
+    }
   }
-  if (b >= c.B) return TokenAt{c.B, 0, 0};
-  const int first = c.q_start[b], end = c.q_start[b + 1];
-  return TokenAt{b, first, end - first};
+  return TokenAt{c.B, 0, 0};
 }
 
 // Tile x of the batch (every sequence's tokens in tiles of `tt`, sequence by
 // sequence): its sequence, its first token in the chunk and the chunk's range.
-// b = B past the last tile.  Ends outside [0, tokens] are clamped, so a tile
-// never names a row outside the buffers.
+// b = B past the last tile.
 struct TileAt {
   int b, first, count, i0;
 };
@@ -109,12 +119,8 @@ __device__ __forceinline__ TileAt find_tile(const ChunkView &c, int64_t x, int t
   int64_t before = 0;
   for (int base = 0; base < c.B; base += 64) {
     const int i = base + lane;
-    int s = 0, e = 0;
-    if (i < c.B) {
-      s = min(max(c.q_start[i], 0), c.tokens);
-      e = min(max(c.q_start[i + 1], s), c.tokens);
-    }
-    const int n = (e - s + tt - 1) / tt;
+    const RowRange r = i < c.B ? row_range(c, i) : RowRange{0, 0};
+    const int n = (r.end - r.first + tt - 1) / tt;
     int incl = n;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -124,7 +130,7 @@ __device__ __forceinline__ TileAt find_tile(const ChunkView &c, int64_t x, int t
     const unsigned long long hit = __ballot(before + incl > x);
     if (hit) {
       const int l = __builtin_ctzll(hit);
-      const int fs = __shfl(s, l), fe = __shfl(e, l), fi = __shfl(incl - n, l);
+      const int fs = __shfl(r.first, l), fe = __shfl(r.end, l), fi = __shfl(incl - n, l);
       return TileAt{base + l, fs, fe - fs, (int)(x - before - fi) * tt};
     }
     before += __shfl(incl, 63);

@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void k_rope_append(RopeArgs a) {
   for (int it = tid; it < TT * H * units; it += kThreads) {
     const int u = it % units, rest = it / units, w = rest / H, h = rest - w * H;
     const int t = t0 + w, b = seq[w];
-    if (b >= a.ch.B) continue;  // rows behind the last sequence stay as they are
+    if (b >= a.ch.B) continue;  // rows of no sequence stay as they are
     const bool is_q = h < a.Hq, is_k = !is_q && h < a.Hq + a.Hkv;
     if (!is_q && !stored[w]) continue;
     const int hk = is_q ? 0 : is_k ? h - a.Hq : h - a.Hq - a.Hkv;
