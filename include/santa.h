@@ -400,7 +400,9 @@ size_t santa_attend_workspace_size(const santa_shape_t *shape, const santa_kv_t 
  * q, out: [num_tokens, num_q_heads, head_dim] contiguous, 16-byte aligned,
  * rotated as the keys are.  A row that sees no key (a token before position 0)
  * is zero; what hidden keys and values hold, infinities and NaN too, reaches no
- * row.  Contiguous and paged caches, every kv_dtype; kv->k_new and kv->v_new
+ * row.  A NaN in a row's query or in a key or value that it sees makes its
+ * outputs NaN (a value's: those of its feature), an infinite value makes them
+ * infinite or, where its weight rounds to zero, NaN.  Contiguous and paged caches, every kv_dtype; kv->k_new and kv->v_new
  * must be NULL.  santa_set_options: `splits` sets the key splits per tile, the
  * path is ignored. */
 santa_status_t santa_attend_chunk(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,

@@ -568,6 +568,20 @@ __device__ __forceinline__ Scale score_scale(const AttendArgs &a, float2 sc) {
   return c == 0.0f ? Scale{1.0f, false, true} : Scale{fabsf(c), c < 0.0f, false};
 }
 
+// A row's maximum as waves and splits give it to the join beside their sum l, in
+// log2 units.  -inf: no score here, neither the sum nor the outputs count.  A NaN
+// score shows in no maximum; the sum that it makes NaN stands above every other,
+// or the join would leave it out beside larger scores, or as a split without any.
+__device__ __forceinline__ float join_max(const RowState &st, float l, float c) {
+  return l != l ? kInf : st.m == -kInf ? -kInf : st.m * c;
+}
+// A split's weight under the maximum of all; negative: it has none and is left out.
+// (One that rounds to zero is not left out: zero times its outputs is NaN where
+// they are not finite.)
+__device__ __forceinline__ float join_weight(float split_max, float top) {
+  return split_max == -kInf ? -1.0f : fast_exp2(split_max - top);
+}
+
 // Adds the non-finite values of keys [lo, hi) that a row sees to N of its
 // features from d on: add(i, value).  (Adding one that the sum has already changes
 // nothing: they absorb.)  A slow loop for a cache that holds such values.
@@ -675,8 +689,9 @@ __device__ __forceinline__ void many_tile(const AttendArgs &a, const Work &w, ch
   if (a.T == 1) {
     f = l > 0.0f || l != l ? sc.y / l : 0.0f;  // a row that sees nothing is zero
   } else {
-    if (h == 0) a.stat[at] = make_float2(st.m == -kInf ? -kInf : st.m * scale.c, l);
-    if (st.m == -kInf) return;  // (nothing seen here: the statistics say so)
+    const float m = join_max(st, l, scale.c);
+    if (h == 0) a.stat[at] = make_float2(m, l);
+    if (m == -kInf) return;  // (nothing seen here: the statistics say so)
   }
 #pragma unroll
   for (int n = 0; n < 4; ++n)
@@ -787,7 +802,7 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
   // join the waves: out = sum_w 2^(m_w - m) O_w / sum_w 2^(m_w - m) l_w
   const float l = xor32_sum(st.l);
   if (h == 0) {
-    wm[wave][r] = st.m == -kInf ? -kInf : st.m * scale.c;
+    wm[wave][r] = join_max(st, l, scale.c);
     wl[wave][r] = l;
   }
   if (lane == 0) {
@@ -868,8 +883,8 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
   for (int r3 = wave; r3 < w.rows; r3 += 4) {
     const int64_t base = w.out_row - (int64_t)w.t * kFewRows + r3;  // split 0's
     const float2 s = lane < a.T ? ld_coherent(a.stat + base + (int64_t)lane * kFewRows) : make_float2(-kInf, 0.0f);
-    const float top = wave_max(s.x), u = s.x == -kInf ? 0.0f : fast_exp2(s.x - top);
-    const float total = wave_sum(u == 0.0f ? 0.0f : u * s.y);
+    const float u = join_weight(s.x, wave_max(s.x));
+    const float total = wave_sum(u < 0.0f ? 0.0f : u * s.y);
     float2 o = make_float2(0, 0);
 #pragma unroll 1
     for (int t = 0; t < a.T; t += 8) {
@@ -879,8 +894,8 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
         y[j] = ld_coherent(reinterpret_cast<const float2 *>(a.part + (base + (int64_t)min(t + j, a.T - 1) * kFewRows) * kHeadDim) + lane);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float uj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u), min(t + j, 63)));  // (0 past the last)
-        if (t + j < a.T && uj != 0.0f) o = make_float2(fmaf(uj, y[j].x, o.x), fmaf(uj, y[j].y, o.y));
+        const float uj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u), min(t + j, 63)));
+        if (t + j < a.T && !(uj < 0.0f)) o = make_float2(fmaf(uj, y[j].x, o.x), fmaf(uj, y[j].y, o.y));
       }
     }
     const float g = total > 0.0f || total != total ? sc.y / total : 0.0f;
@@ -931,8 +946,8 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
     m = wave_max(m);
 #pragma unroll
     for (int k = 0; k < MS; ++k) {
-      s[k].x = s[k].x == -kInf ? 0.0f : fast_exp2(s[k].x - m);  // 0: the split holds no key that the row sees
-      l += s[k].x == 0.0f ? 0.0f : s[k].x * s[k].y;
+      s[k].x = join_weight(s[k].x, m);
+      l += s[k].x < 0.0f ? 0.0f : s[k].x * s[k].y;
     }
     l = wave_sum(l);
     float4 o = make_float4(0, 0, 0, 0);
@@ -945,13 +960,13 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int tt = t + 2 * j + odd;
-          f[j] = __shfl(s[k].x, tt);  // (0 past the last split)
+          f[j] = __shfl(s[k].x, tt);  // (negative past the last split)
           const int64_t at_row = base + (int64_t)min(64 * k + tt, a.T - 1) * ROWS;
           y[j] = reinterpret_cast<const float4 *>(a.part + at_row * kHeadDim)[lane & 31];
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (f[j] == 0.0f) continue;  // (a split of weight 0 may not have written its rows)
+          if (f[j] < 0.0f) continue;  // (a split without scores may not have written its rows)
           o = make_float4(fmaf(f[j], y[j].x, o.x), fmaf(f[j], y[j].y, o.y), fmaf(f[j], y[j].z, o.z), fmaf(f[j], y[j].w, o.w));
         }
       }
