@@ -102,24 +102,42 @@ struct AQ<float> {
   float4 f[16];  // features 8 s + 4 (l / 32) .. + 3
 };
 
-// `neg`: the negated row (a negative scale becomes a positive one).
-__device__ __forceinline__ void load_rows(AQ<uint16_t> &q, const uint16_t *p, bool valid, bool neg) {
+// Bits of the non-finite elements of two bfloat16.
+__device__ __forceinline__ uint32_t nonfinite2(uint32_t w) {
+  const uint32_t e = w & 0x7f807f80u;
+  return ((e & 0xffffu) == 0x7f80u ? 0xffffu : 0u) | ((e >> 16) == 0x7f80u ? 0xffff0000u : 0u);
+}
+
+// Scale of the scores as a positive factor and what goes into the queries instead:
+// a sign, and a scale of zero as zero times the query (NaN where that is not finite).
+struct Scale {
+  float c;
+  bool neg, zero;
+};
+__device__ __forceinline__ Scale score_scale(float scale_log2, float2 sc) {
+  const float c = scale_log2 * sc.x;
+  return c == 0.0f ? Scale{1.0f, false, true} : Scale{fabsf(c), c < 0.0f, false};
+}
+
+__device__ __forceinline__ void load_rows(AQ<uint16_t> &q, const uint16_t *p, bool valid, const Scale &sc) {
   const int h = (threadIdx.x >> 5) & 1;
-  const uint32_t flip = neg ? 0x80008000u : 0u;
+  const uint32_t flip = sc.neg ? 0x80008000u : 0u;
 #pragma unroll
   for (int s = 0; s < 8; ++s) {
     uint4 w = make_uint4(0, 0, 0, 0);
     if (valid) w = *reinterpret_cast<const uint4 *>(p + 16 * s + 8 * h);
+    if (sc.zero) w = make_uint4(nonfinite2(w.x), nonfinite2(w.y), nonfinite2(w.z), nonfinite2(w.w));  // all bits: NaN
     q.f[s] = __builtin_bit_cast(abf16x8, make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip));
   }
 }
-__device__ __forceinline__ void load_rows(AQ<float> &q, const float *p, bool valid, bool neg) {
+__device__ __forceinline__ void load_rows(AQ<float> &q, const float *p, bool valid, const Scale &sc) {
   const int h = (threadIdx.x >> 5) & 1;
+  const float f = sc.zero ? 0.0f : sc.neg ? -1.0f : 1.0f;
 #pragma unroll
   for (int s = 0; s < 16; ++s) {
     float4 w = make_float4(0, 0, 0, 0);
     if (valid) w = *reinterpret_cast<const float4 *>(p + 8 * s + 4 * h);
-    q.f[s] = neg ? make_float4(-w.x, -w.y, -w.z, -w.w) : w;
+    q.f[s] = make_float4(w.x * f, w.y * f, w.z * f, w.w * f);
   }
 }
 
@@ -207,12 +225,6 @@ __device__ __forceinline__ float value32(const char *V, int t, int n, int i) {
   const int lane = threadIdx.x & 63, d = lane & 31, h = lane >> 5;
   const char *col = V + (32 * t + 4 * h) * lds_row<float>() + (((8 * n + (d >> 2)) ^ (h << 3)) << 4) + (d & 3) * 4;
   return *reinterpret_cast<const float *>(col + (8 * (i >> 2) + (i & 3)) * lds_row<float>());
-}
-
-// Bits of the non-finite elements of two bfloat16.
-__device__ __forceinline__ uint32_t nonfinite2(uint32_t w) {
-  const uint32_t e = w & 0x7f807f80u;
-  return ((e & 0xffffu) == 0x7f80u ? 0xffffu : 0u) | ((e >> 16) == 0x7f80u ? 0xffff0000u : 0u);
 }
 
 // The weights over NB blocks of keys, as operands.
@@ -556,18 +568,6 @@ __device__ __forceinline__ void store4(uint16_t *p, float4 v) {
 }
 __device__ __forceinline__ void store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
 
-// Scale of the scores as a non-negative factor and the sign that goes into the
-// queries; with a factor of 0 the queries are zeroed instead.
-struct Scale {
-  float c;
-  bool neg, zero;
-};
-template <typename E>
-__device__ __forceinline__ Scale score_scale(const AttendArgs &a, float2 sc) {
-  const float c = a.scale_log2 * sc.x;
-  return c == 0.0f ? Scale{1.0f, false, true} : Scale{fabsf(c), c < 0.0f, false};
-}
-
 // A row's maximum as waves and splits give it to the join beside their sum l, in
 // log2 units.  -inf: no score here, neither the sum nor the outputs count.  A NaN
 // score shows in no maximum; the sum that it makes NaN stands above every other,
@@ -632,9 +632,9 @@ __device__ __forceinline__ void many_tile(const AttendArgs &a, const Work &w, ch
   const int r = 32 * wave + (lane & 31);
   const Row row = tile_row(a, w, r);
   const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
-  const Scale scale = score_scale<E>(a, sc);
+  const Scale scale = score_scale(a.scale_log2, sc);
   AQ<L> q;
-  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
+  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid, scale);
   // a tile is whole if every row sees all of its keys
   const RowSight first = tile_sight(a, w, 0), last = tile_sight(a, w, w.rows - 1);
   const int all_hi = min(first.hi, w.v_end);
@@ -757,9 +757,9 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
   }
   const Row row = tile_row(a, w, r);
   const float2 sc = kv_scales<E>(a.kv, w.at.b, w.kvh, a.Hkv);
-  const Scale scale = score_scale<E>(a, sc);
+  const Scale scale = score_scale(a.scale_log2, sc);
   AQ<L> q;
-  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid && !scale.zero, scale.neg);
+  load_rows(q, static_cast<const L *>(a.q) + row.at, row.valid, scale);
   const RowSight first = tile_sight(a, w, 0), last = tile_sight(a, w, w.rows - 1);
   RowSight see = row.see;
   see.hi = min(see.hi, end);
