@@ -313,8 +313,8 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
   // keys: 147 at 1, 19.5 at 32).  Grids past one workgroup per CU take a whole
   // second one or none (32k keys: 256 workgroups 32.0, 384 37.6, 512 37.2; two
   // tiles of them 57.6, 44.4, 40.1).
-  const int64_t groups = p.tiles * p.Hkv;
-  // (the tiles to expect, where the caller says how long a sequence's chunk may be)
+  // (the tiles to expect, where the caller says how long a sequence's chunk may be; only
+  // these are split and have partial results, however many rows the buffers hold)
   p.grid_tiles = std::min(p.tiles, n * ((longest + p.tile_tokens - 1) / p.tile_tokens));
   const int64_t busy = p.grid_tiles * p.Hkv;
   const double root = std::sqrt((double)keys);
@@ -337,9 +337,9 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
   // (us, last split / launch, window of 1024: one sequence of G = 4 11.2 / 12.0, of
   // G = 8 12.0 / 11.9, 16 of G = 4 17.7 / 18.9, of G = 8 19.8 / 18.9; 32k keys,
   // G = 4 27.3 / 27.9, G = 8 31.0 / 27.8; two tokens of G = 4 29.2 / 28.2).
-  p.join = p.few && p.T > 1 && p.T <= 64 && longest * p.G <= 4 && groups <= santa::kSyncRowsMax;
+  p.join = p.few && p.T > 1 && p.T <= 64 && longest * p.G <= 4 && busy <= santa::kSyncRowsMax;
   if (p.T > 1) {
-    const size_t rows = (size_t)groups * p.T * p.rows;
+    const size_t rows = (size_t)busy * p.T * p.rows;
     p.off_stat = take(rows * 8);
     p.off_part = take(rows * santa::kHeadDim * 4);
   }
@@ -403,7 +403,7 @@ santa_status_t attend(const void *q, const santa_kv_t *kv, const santa_shape_t *
   if (!std::isfinite(scale)) return fail(SANTA_ERR_INVALID_ARG, "scale must be finite");
   const santa::AttendPlan p = make_attend_plan(sh, kv, ch, win);
   // a launch counts its threads in 32 bits: 256 per split of a tile, 64 per row that is joined
-  if (p.tiles * p.Hkv * std::max(p.T * santa::kThreads, p.rows * 64) > (int64_t)UINT32_MAX)
+  if (p.grid_tiles * p.Hkv * std::max(p.T * santa::kThreads, p.rows * 64) > (int64_t)UINT32_MAX)
     return fail(SANTA_ERR_UNSUPPORTED, "too many tokens times KV heads for one launch");
   s = check_ws(p.total, ws, ws_bytes);
   if (s != SANTA_OK) return s;

@@ -498,14 +498,16 @@ __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0
 // 8 KV heads each XCD works on one head's keys), then split, then tile from
 // the last to the first: in a chunk the later tiles see more keys.  The grid has
 // the tiles to expect; where a batch may have more (MORE: rows enough for chunks
-// longer than max_tokens says), each workgroup goes on with every grid_tiles-th
-// one.  A grid for all that there may be would spend its time on empty workgroups:
+// longer than max_tokens says), each workgroup goes on with the others in turn, a
+// tile at a time and unsplit, so that only the tiles to expect need room for
+// partial results: the (split, tile) workgroups of a KV head share out the rest.  A grid for all that there may be would spend its time on empty workgroups:
 // one token with 2000 padding rows over 2k keys 13.7 us, 91.7 with a workgroup for
 // every tile that the rows could make.  (Without the loop 11.1 us for 12.0 in one
 // user's window.)
 struct Work {
   TileAt at;
-  int kvh, t, rows, p_lo;  // rows: valid ones; p_lo: position of the tile's first token
+  int kvh, rows, p_lo;     // rows: valid ones; p_lo: position of the tile's first token
+  int t, T;                // split, of how many
   int v_begin, v_end;
   KeyMap km;
   int64_t group;           // number of the tile and KV head
@@ -517,7 +519,13 @@ __device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile
   const uint32_t id = blockIdx.x, y = id / (uint32_t)a.Hkv, z = y / (uint32_t)a.T;
   w.kvh = (int)(id - y * a.Hkv);
   w.t = (int)(y - z * a.T);
-  const int64_t x = a.grid_tiles - 1 - (int64_t)z + turn * a.grid_tiles;
+  w.T = a.T;
+  int64_t x = a.grid_tiles - 1 - (int64_t)z;
+  if (turn) {
+    x += ((int64_t)(turn - 1) * a.T + w.t + 1) * a.grid_tiles;
+    w.t = 0;
+    w.T = 1;
+  }
   w.any = x < a.tiles;
   if (!w.any) return w;
   const TileAt at = find_tile(a.ch, x, a.tile_tokens);
@@ -525,14 +533,14 @@ __device__ __forceinline__ Work find_work(const AttendArgs &a, int rows_per_tile
   w.at = TileAt{uniform(at.b), uniform(at.first), uniform(at.count), uniform(at.i0)};
   w.any = w.at.b < a.ch.B;
   w.group = x * a.Hkv + w.kvh;
-  w.out_row = (w.group * a.T + w.t) * rows_per_tile;
+  w.out_row = (w.group * w.T + w.t) * rows_per_tile;  // (unused where a tile is not split)
   if (!w.any) return w;
   const int L = uniform(seq_len(a.kv, w.at.b)), n = min(a.tile_tokens, w.at.count - w.at.i0);
   w.rows = n << a.g_log2;
   w.p_lo = L - w.at.count + w.at.i0;
   // (a chunk longer than its context: tokens before position 0 see nothing)
   w.km = w.p_lo + n - 1 < 0 ? KeyMap{0, 0, 0, 0, 0} : key_map(max(w.p_lo, 0), w.p_lo + n - 1, a.window, a.sinks);
-  const int len = ((w.km.nv + a.T - 1) / a.T + a.step - 1) / a.step * a.step;
+  const int len = ((w.km.nv + w.T - 1) / w.T + a.step - 1) / a.step * a.step;
   w.v_begin = min(w.t * len, w.km.nv);
   w.v_end = min(w.v_begin + len, w.km.nv);
   return w;
@@ -686,7 +694,7 @@ __device__ __forceinline__ void many_tile(const AttendArgs &a, const Work &w, ch
   if (!row.valid) return;
   const int64_t at = w.out_row + r;
   float f = 1.0f;
-  if (a.T == 1) {
+  if (w.T == 1) {
     f = l > 0.0f || l != l ? sc.y / l : 0.0f;  // a row that sees nothing is zero
   } else {
     const float m = join_max(st, l, scale.c);
@@ -699,7 +707,7 @@ __device__ __forceinline__ void many_tile(const AttendArgs &a, const Work &w, ch
     for (int g = 0; g < 4; ++g) {
       const float4 x = make_float4(st.o[n][4 * g] * f, st.o[n][4 * g + 1] * f, st.o[n][4 * g + 2] * f, st.o[n][4 * g + 3] * f);
       const int d = 32 * n + 8 * g + 4 * h;
-      if (a.T == 1) store4(static_cast<L *>(a.out) + row.at + d, x);
+      if (w.T == 1) store4(static_cast<L *>(a.out) + row.at + d, x);
       else *reinterpret_cast<float4 *>(a.part + at * kHeadDim + d) = x;
     }
   if (bad_lo < bad_hi) {
@@ -708,7 +716,7 @@ __device__ __forceinline__ void many_tile(const AttendArgs &a, const Work &w, ch
       L *out = static_cast<L *>(a.out) + row.at + d;
       float *part = a.part + at * kHeadDim + d;
       add_nonfinite<E, PAGED, 4>(a, w, see, bad_lo, bad_hi, d, [&](int i, float x) {
-        if (a.T == 1) add_to(out + i, x);
+        if (w.T == 1) add_to(out + i, x);
         else add_to(part + i, x);
       });
     }
@@ -830,7 +838,7 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
     for (int i = 0; i < 4; ++i) mm = fmaxf(mm, wm[i][r2]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) ll += wm[i][r2] == -kInf ? 0.0f : fast_exp2(wm[i][r2] - mm) * wl[i][r2];
-    const float g = a.T > 1 ? 1.0f : ll > 0.0f || ll != ll ? sc.y / ll : 0.0f;
+    const float g = w.T > 1 ? 1.0f : ll > 0.0f || ll != ll ? sc.y / ll : 0.0f;
     float x[16];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -848,7 +856,7 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
       if (bad[i][0] < bad[i][1])
         add_nonfinite<E, PAGED, 16>(a, w, row2.see, bad[i][0], bad[i][1], 16 * d0, [&](int j, float y) { x[j] += y; });
     const int64_t at = w.out_row + r2;
-    if (a.T == 1) {
+    if (w.T == 1) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         store4(static_cast<L *>(a.out) + row2.at + 16 * d0 + 4 * k,
@@ -866,7 +874,7 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
       for (int k = 0; k < 8; ++k) st_coherent(to + k, make_float2(x[2 * k], x[2 * k + 1]));
     }
   }
-  if (a.T == 1 || !a.sync) return;
+  if (w.T == 1 || !a.sync) return;
 
   // The tile's last split joins them all, a wave per row: every split has stored
   // its part, coherently, before it counts itself; the last one sees T - 1 before
@@ -876,26 +884,26 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
   __syncthreads();
   if (tid == 0) {
     rank = (int)__hip_atomic_fetch_add(count, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (rank == a.T - 1) __hip_atomic_store(count, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (rank == w.T - 1) __hip_atomic_store(count, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  if (rank != a.T - 1) return;
+  if (rank != w.T - 1) return;
   for (int r3 = wave; r3 < w.rows; r3 += 4) {
     const int64_t base = w.out_row - (int64_t)w.t * kFewRows + r3;  // split 0's
-    const float2 s = lane < a.T ? ld_coherent(a.stat + base + (int64_t)lane * kFewRows) : make_float2(-kInf, 0.0f);
+    const float2 s = lane < w.T ? ld_coherent(a.stat + base + (int64_t)lane * kFewRows) : make_float2(-kInf, 0.0f);
     const float u = join_weight(s.x, wave_max(s.x));
     const float total = wave_sum(u < 0.0f ? 0.0f : u * s.y);
     float2 o = make_float2(0, 0);
 #pragma unroll 1
-    for (int t = 0; t < a.T; t += 8) {
+    for (int t = 0; t < w.T; t += 8) {
       float2 y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        y[j] = ld_coherent(reinterpret_cast<const float2 *>(a.part + (base + (int64_t)min(t + j, a.T - 1) * kFewRows) * kHeadDim) + lane);
+        y[j] = ld_coherent(reinterpret_cast<const float2 *>(a.part + (base + (int64_t)min(t + j, w.T - 1) * kFewRows) * kHeadDim) + lane);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float uj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u), min(t + j, 63)));
-        if (t + j < a.T && !(uj < 0.0f)) o = make_float2(fmaf(uj, y[j].x, o.x), fmaf(uj, y[j].y, o.y));
+        if (t + j < w.T && !(uj < 0.0f)) o = make_float2(fmaf(uj, y[j].x, o.x), fmaf(uj, y[j].y, o.y));
       }
     }
     const float g = total > 0.0f || total != total ? sc.y / total : 0.0f;
@@ -916,7 +924,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(few_wg
   }
 }
 
-// Joins the splits' partial results, a wave per (KV head, row of a tile): lane i
+// Joins the splits' partial results, a wave per (KV head, row of a grid tile): lane i
 // takes split i's statistics (and i + 64's, ..), then the half-waves take the even
 // and the odd splits' rows, four features per lane, several rows in flight.
 template <typename E, int ROWS>
@@ -928,54 +936,51 @@ __global__ __launch_bounds__(kThreads) void k_attend_merge(AttendArgs a) {
   const int r = (int)(id % ROWS);
   const uint32_t y = id / ROWS, z = y / (uint32_t)a.Hkv;
   const int kvh = (int)(y - z * a.Hkv);
+  const TileAt at = find_tile(a.ch, z, a.tile_tokens);
+  if (at.b >= a.ch.B) return;
+  const int i = r >> a.g_log2;
+  if (i >= min(a.tile_tokens, at.count - at.i0)) return;
+  const int64_t base = ((int64_t)z * a.Hkv + kvh) * a.T * ROWS + r;
+  float2 s[MS];
+  float m = -kInf, l = 0.0f;
+#pragma unroll
+  for (int k = 0; k < MS; ++k) {
+    const int t = 64 * k + lane;
+    s[k] = t < a.T ? a.stat[base + (int64_t)t * ROWS] : make_float2(-kInf, 0.0f);
+    m = fmaxf(m, s[k].x);
+  }
+  m = wave_max(m);
+#pragma unroll
+  for (int k = 0; k < MS; ++k) {
+    s[k].x = join_weight(s[k].x, m);
+    l += s[k].x < 0.0f ? 0.0f : s[k].x * s[k].y;
+  }
+  l = wave_sum(l);
+  float4 o = make_float4(0, 0, 0, 0);
+#pragma unroll
+  for (int k = 0; k < MS; ++k) {
 #pragma unroll 1
-  for (int64_t x = z; x < a.tiles; x += a.grid_tiles) {
-    const TileAt at = find_tile(a.ch, x, a.tile_tokens);
-    if (at.b >= a.ch.B) return;
-    const int i = r >> a.g_log2;
-    if (i >= min(a.tile_tokens, at.count - at.i0)) continue;
-    const int64_t base = (x * a.Hkv + kvh) * a.T * ROWS + r;
-    float2 s[MS];
-    float m = -kInf, l = 0.0f;
+    for (int t = 0; t < min(64, a.T - 64 * k); t += 8) {
+      float f[4];
+      float4 y[4];
 #pragma unroll
-    for (int k = 0; k < MS; ++k) {
-      const int t = 64 * k + lane;
-      s[k] = t < a.T ? a.stat[base + (int64_t)t * ROWS] : make_float2(-kInf, 0.0f);
-      m = fmaxf(m, s[k].x);
-    }
-    m = wave_max(m);
+      for (int j = 0; j < 4; ++j) {
+        const int tt = t + 2 * j + odd;
+        f[j] = __shfl(s[k].x, tt);  // (negative past the last split)
+        const int64_t at_row = base + (int64_t)min(64 * k + tt, a.T - 1) * ROWS;
+        y[j] = reinterpret_cast<const float4 *>(a.part + at_row * kHeadDim)[lane & 31];
+      }
 #pragma unroll
-    for (int k = 0; k < MS; ++k) {
-      s[k].x = join_weight(s[k].x, m);
-      l += s[k].x < 0.0f ? 0.0f : s[k].x * s[k].y;
-    }
-    l = wave_sum(l);
-    float4 o = make_float4(0, 0, 0, 0);
-#pragma unroll
-    for (int k = 0; k < MS; ++k) {
-#pragma unroll 1
-      for (int t = 0; t < min(64, a.T - 64 * k); t += 8) {
-        float f[4];
-        float4 y[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int tt = t + 2 * j + odd;
-          f[j] = __shfl(s[k].x, tt);  // (negative past the last split)
-          const int64_t at_row = base + (int64_t)min(64 * k + tt, a.T - 1) * ROWS;
-          y[j] = reinterpret_cast<const float4 *>(a.part + at_row * kHeadDim)[lane & 31];
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (f[j] < 0.0f) continue;  // (a split without scores may not have written its rows)
-          o = make_float4(fmaf(f[j], y[j].x, o.x), fmaf(f[j], y[j].y, o.y), fmaf(f[j], y[j].z, o.z), fmaf(f[j], y[j].w, o.w));
-        }
+      for (int j = 0; j < 4; ++j) {
+        if (f[j] < 0.0f) continue;  // (a split without scores may not have written its rows)
+        o = make_float4(fmaf(f[j], y[j].x, o.x), fmaf(f[j], y[j].y, o.y), fmaf(f[j], y[j].z, o.z), fmaf(f[j], y[j].w, o.w));
       }
     }
-    const float g = l > 0.0f || l != l ? kv_scales<E>(a.kv, at.b, kvh, a.Hkv).y / l : 0.0f;
-    o = make_float4(xor32_sum(o.x) * g, xor32_sum(o.y) * g, xor32_sum(o.z) * g, xor32_sum(o.w) * g);
-    const int64_t row = (int64_t)(at.first + at.i0 + i) * a.Hq + (kvh << a.g_log2) + r - (i << a.g_log2);
-    if (!odd) store4(static_cast<L *>(a.out) + row * kHeadDim + 4 * lane, o);
   }
+  const float g = l > 0.0f || l != l ? kv_scales<E>(a.kv, at.b, kvh, a.Hkv).y / l : 0.0f;
+  o = make_float4(xor32_sum(o.x) * g, xor32_sum(o.y) * g, xor32_sum(o.z) * g, xor32_sum(o.w) * g);
+  const int64_t row = (int64_t)(at.first + at.i0 + i) * a.Hq + (kvh << a.g_log2) + r - (i << a.g_log2);
+  if (!odd) store4(static_cast<L *>(a.out) + row * kHeadDim + 4 * lane, o);
 }
 
 // Few rows: a K and a V slot per wave, and at the end the waves' outputs.  Many: two tiles of K and of V.

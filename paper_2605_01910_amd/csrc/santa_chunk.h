@@ -42,13 +42,13 @@ struct AttendPlan {
   int rows;           // query rows (tokens x group) per tile
   int tile_tokens;    // tokens per tile: rows / G
   int64_t tiles;      // upper bound of the batch's tiles per KV head
-  int64_t grid_tiles; // tiles to expect: the grid's; a workgroup takes every grid_tiles-th one
-  int T;              // key splits per tile; 1: no partial results
+  int64_t grid_tiles; // tiles to expect: the grid's; its workgroups take any others too, unsplit
+  int T;              // key splits per tile of the grid; 1: no partial results
   int step;           // split lengths are multiples of this
   int join;           // a tile's last split joins its splits (few rows); 0: a launch of its own
   size_t off_sync;    // the shared head's counters (Plan::off_sync)
-  size_t off_stat;    // float2 [tiles * Hkv * T * rows] (max in log2 units, sum)
-  size_t off_part;    // float [tiles * Hkv * T * rows * 128]
+  size_t off_stat;    // float2 [grid_tiles * Hkv * T * rows] (max in log2 units, sum)
+  size_t off_part;    // float [grid_tiles * Hkv * T * rows * 128]
   size_t total;
 };
 
