@@ -166,8 +166,11 @@ static hipError_t launch_rope_e(const RopeArgs &a, hipStream_t st) {
   void *params[] = {const_cast<RopeArgs *>(&a)};
   // Four tokens per workgroup pay where one has too few items to fill it, on long
   // chunks (us, one / four: 10 heads 2048 tokens 4.6 / 5.2, 4096 7.5 / 6.2, 16384
-  // 24.1 / 16.9; 48 heads 1024 6.4 / 8.0, 4096 19.3 / 18.7, 16384 77 / 81).
-  const bool one = a.ch.tokens < 4096 || (a.Hq + 2 * a.Hkv) * (kHeadDim / 16) >= kThreads;
+  // 24.1 / 16.9; 48 heads 1024 6.4 / 8.0, 4096 19.3 / 18.7, 16384 77 / 81).  A launch
+  // counts its threads in 32 bits (and wraps without an error): 2^24 workgroups are
+  // too many.
+  const bool one = a.ch.tokens < 4096 ||
+                   ((a.Hq + 2 * a.Hkv) * (kHeadDim / 16) >= kThreads && a.ch.tokens < (1 << 24));
   const void *fn = one ? (const void *)k_rope_append<Q, E, 1> : (const void *)k_rope_append<Q, E, 4>;
   return hipExtLaunchKernel(fn, dim3(one ? a.ch.tokens : (a.ch.tokens + 3) / 4), dim3(kThreads), params, 0, st,
                             tm.start, tm.stop, 0);

@@ -60,3 +60,19 @@ def test_four_tokens_a_workgroup(case, queries, R, interleaved):
         bt.put(bt.v, b, p, bt.rows(before[1], b, p))
     for cache, old in ((bt.k, before[0]), (bt.v, before[1])):   # nothing else of the cache changed
         assert torch.equal(torch.nan_to_num(cache.float(), 9), torch.nan_to_num(old.float(), 9))
+
+
+def test_more_rows_than_a_launch_has_threads():
+    """2^24 rows and more of 32 heads: one workgroup of 256 threads per row would pass 32 bits."""
+    T = 2 ** 24 + 1
+    bt = Batch([(4, 50)], Hq=16, Hkv=16, seed=52)
+    rows = torch.empty(T, 16, 128, dtype=bt.dtype, device="cuda")
+    rows[-4:] = new_rows(bt, False)[1]
+    ends = torch.tensor([T - 4, T], dtype=torch.int32, device="cuda")
+    before = bt.v.clone()
+    S.santa_rope_append(None, rows, rows, bt.kv(), bt.shape(), S.chunk_of(ends, T), None, None)
+    torch.cuda.synchronize()
+    assert torch.equal(bt.k[0, 46:], rows[-4:]) and torch.equal(bt.v[0, 46:], rows[-4:])
+    assert torch.equal(bt.v[0, :46], before[0, :46])
+    del rows
+    torch.cuda.empty_cache()
