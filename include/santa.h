@@ -402,7 +402,10 @@ size_t santa_attend_workspace_size(const santa_shape_t *shape, const santa_kv_t 
  * is zero; what hidden keys and values hold, infinities and NaN too, reaches no
  * row.  A NaN in a row's query or in a key or value that it sees makes its
  * outputs NaN (a value's: those of its feature), an infinite value makes them
- * infinite or, where its weight rounds to zero, NaN.  Contiguous and paged caches, every kv_dtype; kv->k_new and kv->v_new
+ * infinite or, where its weight rounds to zero, NaN.  Scores, sums and outputs are
+ * kept in float32; over bfloat16 and FP8 caches a weight is rounded before it
+ * multiplies its value, by up to 2^-14 of itself where max_tokens (num_tokens, if
+ * unknown) times the group is at most 32, by up to 2^-8 (bfloat16) beyond.  Contiguous and paged caches, every kv_dtype; kv->k_new and kv->v_new
  * must be NULL.  santa_set_options: `splits` sets the key splits per tile, the
  * path is ignored. */
 santa_status_t santa_attend_chunk(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,

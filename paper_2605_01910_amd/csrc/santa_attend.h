@@ -227,28 +227,42 @@ __device__ __forceinline__ float value32(const char *V, int t, int n, int i) {
   return *reinterpret_cast<const float *>(col + (8 * (i >> 2) + (i & 3)) * lds_row<float>());
 }
 
-// The weights over NB blocks of keys, as operands.
-template <typename L, int NB>
+// The weights over NB blocks of keys, as operands.  The matrix instruction that
+// takes bfloat16 values takes bfloat16 weights, rounded by at most 2^-8 of a weight
+// (nearest even; their sum keeps 32 bits).  FINE: in two parts, off by 2^-14: what
+// the first leaves is a second operand.  The first lies half a step to one and a
+// half below the weight, so that both are positive: an infinite value is infinite
+// times either.  Few rows wait for memory and take it (us, one part / two: one window
+// of 1024 keys 11.2 / 11.6, 64 of 4096 169.0 / 169.1, 16 in FP8 21.5 / 22.2, drafted
+// tokens 71.3 / 70.3), full tiles wait for the products and do not (512 tokens at 32k
+// 317 / 424, an 8k prompt 597 / 797, a window of 1024 over 2k tokens 53.9 / 67.1).
+template <typename L, int NB, bool FINE>
 struct Weights {
-  abf16x8 f[2 * NB];  // nearest even: at most 2^-8 of a weight; the sum of weights keeps 32 bits
+  abf16x8 f[2 * NB], rest[FINE ? 2 * NB : 1];
 };
-template <int NB>
-struct Weights<float, NB> {
+template <int NB, bool FINE>
+struct Weights<float, NB, FINE> {
   af32x16 f[NB];
 };
 
 // O^T += V^T P^T over the tile at V (rows of type L).
-template <typename L, int NB>
-__device__ __forceinline__ void add_values(RowState &st, const Weights<QE<L>, NB> &p, const char *V, L) {
+template <typename L, int NB, bool FINE>
+__device__ __forceinline__ void add_values(RowState &st, const Weights<QE<L>, NB, FINE> &p, const char *V, L) {
   const int h = (threadIdx.x >> 5) & 1;
   if constexpr (sizeof(L) <= 2) {
 #pragma unroll
-    for (int b = 0; b < 2 * NB; ++b)
+    for (int b = 0; b < 2 * NB; ++b) {
+      abf16x8 w[4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        const abf16x8 w = __builtin_bit_cast(abf16x8, value_operand(V, 16 * b + 4 * h, n, L{}));
-        st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p.f[b], st.o[n], 0, 0, 0);
+        w[n] = __builtin_bit_cast(abf16x8, value_operand(V, 16 * b + 4 * h, n, L{}));
+        st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[n], p.f[b], st.o[n], 0, 0, 0);
       }
+      if constexpr (FINE)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+          st.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[n], p.rest[b], st.o[n], 0, 0, 0);
+    }
   } else {
 #pragma unroll
     for (int t = 0; t < NB; ++t)
@@ -366,15 +380,24 @@ __device__ __forceinline__ void weigh(RowState &st, af32x16 (&s)[NB], float c) {
     }
   st.l += l[0] + l[1];
 }
-template <int NB>
-__device__ __forceinline__ void pack(Weights<uint16_t, NB> &w, const af32x16 (&s)[NB]) {
+template <int NB, bool FINE>
+__device__ __forceinline__ void pack(Weights<uint16_t, NB, FINE> &w, const af32x16 (&s)[NB]) {
 #pragma unroll
   for (int b = 0; b < 2 * NB; ++b)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w.f[b][i] = (__bf16)s[b / 2][8 * (b & 1) + i];
+    for (int i = 0; i < 8; ++i) {
+      const float x = s[b / 2][8 * (b & 1) + i];
+      if constexpr (FINE) {
+        const uint32_t part = __builtin_elementwise_sub_sat(__float_as_uint(x), 0x8000u) & 0xffff0000u;
+        w.f[b][i] = __builtin_bit_cast(__bf16, (uint16_t)(part >> 16));
+        w.rest[b][i] = (__bf16)(x - __uint_as_float(part));
+      } else {
+        w.f[b][i] = (__bf16)x;
+      }
+    }
 }
-template <int NB>
-__device__ __forceinline__ void pack(Weights<float, NB> &w, const af32x16 (&s)[NB]) {
+template <int NB, bool FINE>
+__device__ __forceinline__ void pack(Weights<float, NB, FINE> &w, const af32x16 (&s)[NB]) {
 #pragma unroll
   for (int t = 0; t < NB; ++t) w.f[t] = s[t];
 }
@@ -684,7 +707,7 @@ __device__ __forceinline__ void many_tile(const AttendArgs &a, const Work &w, ch
     const float f = move_reference(st, row_max(s), scale.c);
     if (__any(f != 1.0f)) rescale(st, f);
     weigh(st, s, scale.c);
-    Weights<L, NB> p;
+    Weights<L, NB, false> p;
     pack(p, s);
     add_values(st, p, V, E{});
     turn ^= 1;
@@ -794,7 +817,7 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
     const float f = move_reference(st, row_max(s), scale.c);
     if (__any(f != 1.0f)) rescale(st, f);
     weigh(st, s, scale.c);
-    Weights<L, NB> p;
+    Weights<L, NB, true> p;
     pack(p, s);
     if (more) wait_copies<NL>();
     else wait_copies<0>();
