@@ -455,7 +455,7 @@ def alloc_attend_workspace(shape: santa_shape_t, kv: santa_kv_t, chunk: Optional
     ws = torch.empty(n + 256, dtype=torch.uint8, device=device)
     off = (-ws.data_ptr()) % 256
     ws = ws[off:off + n]
-    santa_workspace_init(ws)
+    _launch(load().santa_workspace_init, (ws,), None, ws.data_ptr(), n)
     return ws
 
 
