@@ -264,6 +264,14 @@ santa_status_t check_ws(const santa::Plan &p, void *ws, size_t ws_bytes) { retur
 
 bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15; }
 
+constexpr int64_t kMaxWorkgroups = UINT32_MAX / santa::kThreads;
+
+// Whether both launches of the plan count their threads in 32 bits (a wave per row that is joined).
+bool attend_fits(const santa::AttendPlan &p) {
+  const int64_t groups = p.grid_tiles * p.Hkv;
+  return groups * p.T <= kMaxWorkgroups && (p.T == 1 || p.join || groups * p.rows / (santa::kThreads / 64) <= kMaxWorkgroups);
+}
+
 // Chunk of new tokens (NULL: one per sequence).
 santa_status_t check_chunk(const santa_chunk_t *ch, const santa_shape_t *sh, santa_chunk_t *out) {
   *out = ch ? *ch : santa_chunk_t{nullptr, sh->batch, 1};
@@ -316,6 +324,8 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
   // (the tiles to expect, where the caller says how long a sequence's chunk may be; only
   // these are split and have partial results, however many rows the buffers hold)
   p.grid_tiles = std::min(p.tiles, n * ((longest + p.tile_tokens - 1) / p.tile_tokens));
+  // (a launch counts its threads in 32 bits: the grid's workgroups take what is past that too)
+  p.grid_tiles = std::max<int64_t>(1, std::min(p.grid_tiles, kMaxWorkgroups / p.Hkv));
   const int64_t busy = p.grid_tiles * p.Hkv;
   const double root = std::sqrt((double)keys);
   const bool heavy = p.elem == 1 && !p.few;
@@ -402,9 +412,7 @@ santa_status_t attend(const void *q, const santa_kv_t *kv, const santa_shape_t *
   if (misaligned(q) || misaligned(out)) return fail(SANTA_ERR_UNSUPPORTED, "q and out must be 16-byte aligned");
   if (!std::isfinite(scale)) return fail(SANTA_ERR_INVALID_ARG, "scale must be finite");
   const santa::AttendPlan p = make_attend_plan(sh, kv, ch, win);
-  // a launch counts its threads in 32 bits: 256 per split of a tile, 64 per row that is joined
-  if (p.grid_tiles * p.Hkv * std::max(p.T * santa::kThreads, p.rows * 64) > (int64_t)UINT32_MAX)
-    return fail(SANTA_ERR_UNSUPPORTED, "too many tokens times KV heads for one launch");
+  if (!attend_fits(p)) return fail(SANTA_ERR_UNSUPPORTED, "too many KV heads or splits for one launch");
   s = check_ws(p.total, ws, ws_bytes);
   if (s != SANTA_OK) return s;
   santa::AttendArgs a{};

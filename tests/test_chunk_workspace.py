@@ -41,11 +41,19 @@ def test_partial_results_are_bounded(B, rows, most):
                 size(B, n_k, rows, most, Hkv, Hkv) == head
 
 
-def test_launches_that_fit_are_not_refused():
-    """2^25 rows for one token of 128 KV heads: the launch is one tile's.  (The workspace is refused
-    after the launch's size, so that no launch is made here.)"""
-    kv = S.santa_kv_t(16, 16, 0, 128 * 128, 128, None, None, 0, 0, 64)
-    sh, ch = S.santa_shape_t(1, 128, 128, 128, 0), S.santa_chunk_t(16, 2 ** 25, 1)
+@pytest.mark.parametrize("Hq,Hkv,most", [(128, 128, 1), (128, 128, 0), (64, 8, 0), (8, 1, 0), (64, 8, 2 ** 20)])
+def test_long_batches_are_not_refused(Hq, Hkv, most):
+    """2^25 rows, the most that a call may have.  (A missing workspace is refused after the launch's
+    size is, so no launch is made here.)"""
+    kv = S.santa_kv_t(16, 16, 0, Hkv * 128, 128, None, None, 0, 0, 4096)
+    sh, ch = S.santa_shape_t(1, Hq, Hkv, 128, 0), S.santa_chunk_t(16, 2 ** 25, most)
     assert S.load().santa_attend_chunk(16, ref(kv), ref(sh), ref(ch), None, 0.1, 16, None, 0, None) == S.SANTA_ERR_WORKSPACE
-    ch.max_tokens = 0
-    assert S.load().santa_attend_chunk(16, ref(kv), ref(sh), ref(ch), None, 0.1, 16, None, 0, None) == S.SANTA_ERR_UNSUPPORTED
+
+
+def test_launches_that_do_not_fit_are_refused():
+    kv = S.santa_kv_t(16, 16, 0, 0, 128, None, None, 0, 0, 4096)
+    sh = S.santa_shape_t(1, 2 ** 24 + 8, 2 ** 24 + 8, 128, 0)
+    assert S.load().santa_attend_chunk(16, ref(kv), ref(sh), None, None, 0.1, 16, None, 0, None) == S.SANTA_ERR_UNSUPPORTED
+    sh, ch = S.santa_shape_t(4096, 32, 32, 128, 0), S.santa_chunk_t(16, 2 ** 21, 0)
+    with S.options("auto", 256):
+        assert S.load().santa_attend_chunk(16, ref(kv), ref(sh), ref(ch), None, 0.1, 16, None, 0, None) == S.SANTA_ERR_UNSUPPORTED
