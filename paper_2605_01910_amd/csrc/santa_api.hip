@@ -86,17 +86,24 @@ santa_status_t check_shape(const santa_shape_t *sh) {
   return SANTA_OK;
 }
 
+// What a plan takes from the cache: its length and element type.
+santa_status_t check_kv_kind(const santa_kv_t *kv, const santa_shape_t *sh) {
+  if (kv->n_k < 1) return fail(SANTA_ERR_INVALID_ARG, "n_k must be >= 1");
+  if (kv->kv_dtype != SANTA_KV_AS_Q && kv->kv_dtype != SANTA_KV_FP8_E4M3)
+    return fail(SANTA_ERR_INVALID_ARG, "kv_dtype must be SANTA_KV_AS_Q or SANTA_KV_FP8_E4M3");
+  if (kv->kv_dtype == SANTA_KV_FP8_E4M3 && sh->dtype != SANTA_BF16)
+    return fail(SANTA_ERR_UNSUPPORTED, "an FP8 cache needs bfloat16 queries (shape->dtype)");
+  return SANTA_OK;
+}
+
 // decode: the call is a decode step, which reads an FP8 cache on its fused paths only
 santa_status_t check_kv(const santa_kv_t *kv, const santa_shape_t *sh, bool need_k, bool decode = true) {
   if (!kv) return fail(SANTA_ERR_INVALID_ARG, "kv is NULL");
   if ((need_k && !kv->k) || !kv->v) return fail(SANTA_ERR_INVALID_ARG, "kv->k or kv->v is NULL");
-  if (kv->n_k < 1) return fail(SANTA_ERR_INVALID_ARG, "n_k must be >= 1");
-  if (kv->kv_dtype != SANTA_KV_AS_Q && kv->kv_dtype != SANTA_KV_FP8_E4M3)
-    return fail(SANTA_ERR_INVALID_ARG, "kv_dtype must be SANTA_KV_AS_Q or SANTA_KV_FP8_E4M3");
+  const santa_status_t s = check_kv_kind(kv, sh);
+  if (s != SANTA_OK) return s;
   const bool fp8 = kv->kv_dtype == SANTA_KV_FP8_E4M3;
   if (fp8) {
-    if (sh->dtype != SANTA_BF16)
-      return fail(SANTA_ERR_UNSUPPORTED, "an FP8 cache needs bfloat16 queries (shape->dtype)");
     if (!kv->k_scale || !kv->v_scale)
       return fail(SANTA_ERR_INVALID_ARG, "an FP8 cache needs k_scale and v_scale");
     if (kv->k_new || kv->v_new)
@@ -768,10 +775,11 @@ santa_status_t santa_rope_append(const santa_rows_t *rows, const santa_kv_t *kv,
 size_t santa_attend_workspace_size(const santa_shape_t *shape, const santa_kv_t *kv, const santa_chunk_t *chunk,
                                    const santa_window_t *window) {
   santa_chunk_t ch;
-  if (check_shape(shape) != SANTA_OK || !kv || kv->n_k < 1 || check_chunk(chunk, shape, &ch) != SANTA_OK ||
-      check_window(window) != SANTA_OK)
+  if (check_shape(shape) != SANTA_OK || !kv || check_kv_kind(kv, shape) != SANTA_OK ||
+      check_chunk(chunk, shape, &ch) != SANTA_OK || check_window(window) != SANTA_OK)
     return 0;
-  return make_attend_plan(shape, kv, ch, window).total;
+  const santa::AttendPlan p = make_attend_plan(shape, kv, ch, window);
+  return attend_fits(p) ? p.total : 0;
 }
 
 santa_status_t santa_attend_chunk(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,

@@ -57,3 +57,13 @@ def test_launches_that_do_not_fit_are_refused():
     sh, ch = S.santa_shape_t(4096, 32, 32, 128, 0), S.santa_chunk_t(16, 2 ** 21, 0)
     with S.options("auto", 256):
         assert S.load().santa_attend_chunk(16, ref(kv), ref(sh), ref(ch), None, 0.1, 16, None, 0, None) == S.SANTA_ERR_UNSUPPORTED
+
+
+def test_no_size_for_calls_that_are_refused():
+    assert size() > 0 and size(dtype=1) > 0
+    kv = S.santa_kv_t(16, 16, 0, 128, 128, None, None, 0, 0, 4096)
+    for dtype, kv_dtype, fine in ((0, 0, True), (0, 1, True), (1, 0, True), (1, 1, False), (0, 2, False), (0, -1, False)):
+        kv.kv_dtype = kv_dtype
+        sh = S.santa_shape_t(2, 8, 2, 128, dtype)
+        assert (S.load().santa_attend_workspace_size(ref(sh), ref(kv), None, None) > 0) == fine
+    assert size(Hq=2 ** 24 + 8, Hkv=2 ** 24 + 8, n_k=1) == 0
