@@ -373,7 +373,8 @@ typedef struct {
 
 /* Rotary positions and the store into the cache, in one pass: every pair (a, b)
  * of a query or key at position p becomes gain * (a cos - b sin, b cos + a sin)
- * at the angle p * f_i, exact in p for any p; rotated queries go to q_out
+ * at the angle p * f_i, with whole turns left out exactly (off by at most |p| * 2^-60
+ * of a turn, for any p, and by the float32 sine and cosine); rotated queries go to q_out
  * ([num_tokens, num_q_heads, head_dim] contiguous; may be q itself if q is
  * contiguous), rotated keys and the values as they are to the tokens' rows of
  * the cache.  rope = NULL rotates nothing (q and q_out must then be NULL): a

@@ -444,22 +444,25 @@ santa_status_t attend(const void *q, const santa_kv_t *kv, const santa_shape_t *
   return hip_status(santa::launch_attend(p, a, static_cast<hipStream_t>(stream)));
 }
 
-// Turns per position of pair i, before any whole turns are left out.
-double rope_turns(const santa_rope_params_t &r, int i) {
-  const double pi2 = 6.283185307179586476925, R = r.rotary_dim;
-  const double theta = r.scaling == SANTA_ROPE_BASE ? r.theta * std::pow(r.factor, R / (R - 2)) : r.theta;
-  const double f = std::pow(theta, -2.0 * i / R);
-  double keep = 1.0;  // share of the unscaled frequency
-  if (r.scaling == SANTA_ROPE_LINEAR) keep = 0.0;
-  if (r.scaling == SANTA_ROPE_BANDS) keep = (r.original_len * f / pi2 - r.low) / (r.high - r.low);
+// Turns per position of pair i, before any whole turns are left out.  In 64 bits of
+// mantissa: an error of a frequency grows with the position (a double's 2^-53 would
+// be 1e-7 of a turn at 2^30, and more than the sine's 32 bits from 2^24 on).
+long double rope_turns(const santa_rope_params_t &r, int i) {
+  const long double pi2 = 6.283185307179586476925286766559L, R = r.rotary_dim;
+  const long double theta =
+      r.scaling == SANTA_ROPE_BASE ? r.theta * std::pow((long double)r.factor, R / (R - 2)) : (long double)r.theta;
+  const long double f = std::pow(theta, -2 * i / R);
+  long double keep = 1;  // share of the unscaled frequency
+  if (r.scaling == SANTA_ROPE_LINEAR) keep = 0;
+  if (r.scaling == SANTA_ROPE_BANDS) keep = (r.original_len * f / pi2 - r.low) / ((long double)r.high - r.low);
   if (r.scaling == SANTA_ROPE_RAMP) {
-    auto pair = [&](double turns) { return R * std::log(r.original_len / (pi2 * turns)) / (2.0 * std::log(r.theta)); };
-    const double lo = std::max(0.0, std::floor(pair(r.high))), hi = std::min(R - 1.0, std::ceil(pair(r.low)));
-    keep = 1.0 - (i - lo) / std::max(hi - lo, 0.001);
+    auto pair = [&](double turns) { return R * std::log(r.original_len / (pi2 * turns)) / (2 * std::log((long double)r.theta)); };
+    const long double lo = std::max(0.0L, std::floor(pair(r.high))), hi = std::min(R - 1, std::ceil(pair(r.low)));
+    keep = 1 - (i - lo) / std::max(hi - lo, 0.001L);
   }
-  keep = std::min(1.0, std::max(0.0, keep));
+  keep = std::min(1.0L, std::max(0.0L, keep));
   const bool scaled = r.scaling != SANTA_ROPE_PLAIN && r.scaling != SANTA_ROPE_BASE;
-  return (scaled ? f * keep + f / r.factor * (1.0 - keep) : f) / pi2;
+  return (scaled ? f * keep + f / r.factor * (1 - keep) : f) / pi2;
 }
 
 santa_status_t sampled(const void *q, const santa_kv_t *kv, const santa_shape_t *sh, float scale,
@@ -717,10 +720,8 @@ santa_status_t santa_rope_init(const santa_rope_params_t *params, santa_rope_t *
   rope->gain = (float)(r.gain != 0.0 ? r.gain
                        : r.scaling == SANTA_ROPE_RAMP && r.factor > 1.0 ? 0.1 * std::log(r.factor) + 1.0 : 1.0);
   for (int i = 0; i < r.rotary_dim / 2; ++i) {
-    const double turns = rope_turns(r, i);
-    // (a fraction that rounds to a whole turn is one of 0: ldexp of it is 2^64)
-    const double x = std::ldexp(turns - std::floor(turns), 64);
-    rope->step[i] = x < 18446744073709551616.0 ? (uint64_t)x : 0;
+    const long double turns = rope_turns(r, i), x = std::ldexp(turns - std::floor(turns), 64);
+    rope->step[i] = x < 18446744073709551616.0L ? (uint64_t)x : 0;
   }
   return SANTA_OK;
 }

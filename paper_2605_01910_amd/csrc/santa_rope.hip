@@ -41,7 +41,8 @@ __device__ __forceinline__ void store8(uint8_t *p, const float (&f)[8]) {
 
 // cos and sin of position * frequency, times the gain.  The product is taken
 // in whole 2^-64ths of a turn, where leaving out whole turns is the wrap of
-// the multiplication: no error grows with the position.
+// the multiplication: what grows with the position is only the plan's error of a
+// few 2^-64ths.
 __device__ __forceinline__ float2 turn(int64_t pos, uint64_t step, float gain) {
   const uint64_t phase = (uint64_t)pos * step;
   const float half_turns = (float)(int32_t)(phase >> 32) * 0x1p-31f;  // in [-1, 1]
