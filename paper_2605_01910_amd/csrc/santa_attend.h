@@ -37,7 +37,7 @@ typedef __bf16 abf16x2 __attribute__((ext_vector_type(2)));
 typedef short as16x4 __attribute__((ext_vector_type(4)));
 typedef float af32x16 __attribute__((ext_vector_type(16)));
 
-// Element type in LDS: FP8 codes are widened (exactly) on the way in.
+// Element type of q and out.
 template <typename E>
 using LE = QE<E>;
 
@@ -327,10 +327,13 @@ __device__ __forceinline__ bool clean_values(char *V, int tl) {
 }
 
 // The online softmax, in three parts.  The reference m of a row moves only when
-// a score passes it by more than 8 in log2 units: a weight is at most 2^8, which
-// costs 32-bit sums and the weights' rounding nothing, and the output is
+// a score passes it by more than kLag in log2 units, so that the output is
 // rescaled in the first tiles only instead of whenever one of 32 rows finds a
-// new maximum.
+// new maximum.  Weights are taken under m + kLag: none is above 1 (2^8 times a
+// large value would overflow) and the largest is at least 2^-8, which costs 32-bit
+// sums and the weights' rounding nothing.
+constexpr float kLag = 8.0f;
+__device__ __forceinline__ float reference(const RowState &st, float c) { return fmaf(st.m, c, kLag); }
 template <int NB>
 __device__ __forceinline__ void hide(af32x16 (&s)[NB], int v0, const RowSight &rs) {
   const int h = (threadIdx.x >> 5) & 1;
@@ -354,7 +357,7 @@ __device__ __forceinline__ float row_max(const af32x16 (&s)[NB]) {
 // The factor that the output and the sum so far take (1 if the reference stays;
 // no score yet: m is -inf, passed by any score but -inf).
 __device__ __forceinline__ float move_reference(RowState &st, float tm, float c) {
-  const bool move = tm * c > fmaf(st.m, c, 8.0f);
+  const bool move = tm * c > reference(st, c);
   const float f = move ? fast_exp2((st.m - tm) * c) : 1.0f;
   st.m = move ? tm : st.m;
   st.l *= f;
@@ -369,7 +372,7 @@ __device__ __forceinline__ void rescale(RowState &st, float f) {
 // Scores become weights, and their sum the row's.
 template <int NB>
 __device__ __forceinline__ void weigh(RowState &st, af32x16 (&s)[NB], float c) {
-  const float mc = st.m == -kInf ? 0.0f : st.m * c;  // nothing visible yet: every weight is 0
+  const float mc = st.m == -kInf ? 0.0f : reference(st, c);  // nothing visible yet: every weight is 0
   float l[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int t = 0; t < NB; ++t)
@@ -599,12 +602,12 @@ __device__ __forceinline__ void store4(uint16_t *p, float4 v) {
 }
 __device__ __forceinline__ void store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
 
-// A row's maximum as waves and splits give it to the join beside their sum l, in
+// A row's reference as waves and splits give it to the join beside their sum l, in
 // log2 units.  -inf: no score here, neither the sum nor the outputs count.  A NaN
 // score shows in no maximum; the sum that it makes NaN stands above every other,
 // or the join would leave it out beside larger scores, or as a split without any.
-__device__ __forceinline__ float join_max(const RowState &st, float l, float c) {
-  return l != l ? kInf : st.m == -kInf ? -kInf : st.m * c;
+__device__ __forceinline__ float join_reference(const RowState &st, float l, float c) {
+  return l != l ? kInf : st.m == -kInf ? -kInf : reference(st, c);
 }
 // A split's weight under the maximum of all; negative: it has none and is left out.
 // (One that rounds to zero is not left out: zero times its outputs is NaN where
@@ -720,7 +723,7 @@ __device__ __forceinline__ void many_tile(const AttendArgs &a, const Work &w, ch
   if (w.T == 1) {
     f = l > 0.0f || l != l ? sc.y / l : 0.0f;  // a row that sees nothing is zero
   } else {
-    const float m = join_max(st, l, scale.c);
+    const float m = join_reference(st, l, scale.c);
     if (h == 0) a.stat[at] = make_float2(m, l);
     if (m == -kInf) return;  // (nothing seen here: the statistics say so)
   }
@@ -833,7 +836,7 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
   // join the waves: out = sum_w 2^(m_w - m) O_w / sum_w 2^(m_w - m) l_w
   const float l = xor32_sum(st.l);
   if (h == 0) {
-    wm[wave][r] = join_max(st, l, scale.c);
+    wm[wave][r] = join_reference(st, l, scale.c);
     wl[wave][r] = l;
   }
   if (lane == 0) {
@@ -844,7 +847,7 @@ __device__ __forceinline__ void few_tile(const AttendArgs &a, const Work &w, cha
   float m = -kInf;
 #pragma unroll
   for (int i = 0; i < 4; ++i) m = fmaxf(m, wm[i][r]);
-  const float f = st.m == -kInf ? 0.0f : fast_exp2(st.m * scale.c - m);
+  const float f = st.m == -kInf ? 0.0f : fast_exp2(reference(st, scale.c) - m);
   float4 *part = reinterpret_cast<float4 *>(lds);  // [wave][32 quads of features][32 rows]
   if (r < w.rows)
 #pragma unroll

@@ -47,7 +47,7 @@ struct AttendPlan {
   int step;           // split lengths are multiples of this
   int join;           // a tile's last split joins its splits (few rows); 0: a launch of its own
   size_t off_sync;    // the shared head's counters (Plan::off_sync)
-  size_t off_stat;    // float2 [grid_tiles * Hkv * T * rows] (max in log2 units, sum)
+  size_t off_stat;    // float2 [grid_tiles * Hkv * T * rows] (reference in log2 units, sum)
   size_t off_part;    // float [grid_tiles * Hkv * T * rows * 128]
   size_t total;
 };
