@@ -421,8 +421,8 @@ santa_status_t santa_decode_window(const void *q, const santa_kv_t *kv, const sa
 
 /* Profiling hook (not part of the method).  start_event and stop_event are
  * hipEvent_t handles created by the caller with timing enabled.  The next
- * santa_decode_* (or santa_stream_read) call made on the calling thread
- * attaches them to its own kernels: the GPU records start_event when the
+ * santa_decode_*, santa_rope_append or santa_attend_chunk (or santa_stream_read)
+ * call made on the calling thread attaches them to its own kernels: the GPU records start_event when the
  * call's first kernel is
  * dispatched and stop_event when its last kernel completes, so
  * hipEventElapsedTime(start, stop) is the call's execution time on the device

@@ -19,7 +19,7 @@ namespace {
 thread_local std::string g_last_error;
 thread_local santa::CallTimer g_timer;
 
-// Consumes the pending call timer when a decode entry point returns.
+// Consumes the pending call timer when an entry point that launches kernels returns.
 struct TimerScope {
   ~TimerScope() { g_timer = santa::CallTimer{}; }
 };

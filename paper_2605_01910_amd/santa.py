@@ -530,8 +530,8 @@ def santa_stream_read(buf, sink, stream=None) -> None:
 
 
 def santa_time_next_call(start, stop) -> None:
-    """Attach two timing events to the kernels of the next santa_decode_* (or
-    santa_stream_read) call on this thread (start: first kernel dispatched, stop: last kernel done).
+    """Attach two timing events to the kernels of the next santa_decode_*, santa_rope_append,
+    santa_attend_chunk or santa_stream_read call on this thread (start: first kernel dispatched, stop: last kernel done).
     `start`/`stop` are torch.cuda.Event objects that have been recorded at least
     once (so their HIP event exists), raw hipEvent_t handles, or both None."""
     def handle(e):
