@@ -249,10 +249,16 @@ def kt_feature_major(k_t: torch.Tensor) -> santa_kt_t:
 def chunk_of(q_start: Optional[torch.Tensor], num_tokens: int, max_tokens: int = 0) -> santa_chunk_t:
     """New tokens of a batch: sequence b's are rows q_start[b] .. q_start[b + 1] - 1 (int32
     [batch + 1] on the device; None: one token per sequence).  max_tokens: the most tokens a
-    sequence is expected to have (0: unknown)."""
+    sequence is expected to have (0: unknown).  The chunk keeps q_start alive."""
     if q_start is not None and (not q_start.is_cuda or q_start.dtype != torch.int32 or not q_start.is_contiguous()):
         raise TypeError("q_start must be a contiguous int32 CUDA tensor")
-    return santa_chunk_t(None if q_start is None else q_start.data_ptr(), int(num_tokens), int(max_tokens))
+    chunk = santa_chunk_t(None if q_start is None else q_start.data_ptr(), int(num_tokens), int(max_tokens))
+    chunk.tensors = () if q_start is None else (q_start,)
+    return chunk
+
+
+def _chunk_tensors(chunk: Optional[santa_chunk_t]) -> tuple:
+    return getattr(chunk, "tensors", ())  # (none for a chunk made from raw pointers)
 
 
 def window_of(window: int, sinks: int = 0) -> santa_window_t:
@@ -436,7 +442,7 @@ def santa_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
             raise TypeError("positions must be a contiguous int32 tensor with a position per token")
         rows.positions = positions.data_ptr()
     tensors = [x for x in (k, v, q, q_out, positions) if x is not None]
-    _launch(load().santa_rope_append, tensors, stream, rows, kv, shape, chunk, rope,
+    _launch(load().santa_rope_append, tensors + [*_chunk_tensors(chunk)], stream, rows, kv, shape, chunk, rope,
             None if q_out is None else q_out.data_ptr())
 
 
@@ -466,7 +472,7 @@ def santa_attend_chunk(q: torch.Tensor, kv: santa_kv_t, shape: santa_shape_t, ch
     T, dt = shape.batch if chunk is None else chunk.num_tokens, _TORCH_DTYPE[shape.dtype]
     _rows_check("q", q, T, shape.num_q_heads, dt)
     _rows_check("out", out, T, shape.num_q_heads, dt)
-    _launch(load().santa_attend_chunk, (q, out, ws), stream, q.data_ptr(), kv, shape, chunk, window, scale,
+    _launch(load().santa_attend_chunk, (q, out, ws, *_chunk_tensors(chunk)), stream, q.data_ptr(), kv, shape, chunk, window, scale,
             out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 

@@ -1,7 +1,10 @@
 """Calls with tensors on another device than the current one (no GPU: the library is stood in for)."""
 
 import contextlib
+import gc
+import weakref
 
+import pytest
 import torch
 
 from paper_2605_01910_amd import santa as S
@@ -37,3 +40,27 @@ def test_the_workspace_is_cleared_on_its_own_device(monkeypatch):
     ws = S.alloc_attend_workspace(None, None, device="cuda:1")
     assert calls == [(1, 1024, 101)] and current == [0]
     assert ws.numel() == 1024 and ws.data_ptr() % 256 == 0
+
+
+def test_a_chunk_keeps_its_tensor(monkeypatch):
+    """chunk_of over a temporary: the prefix sums live as long as the chunk, and a call refuses them on
+    another device than its rows."""
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)
+    ends = torch.tensor([0, 5], dtype=torch.int32)
+    gone = weakref.ref(ends)
+    chunk = S.chunk_of(ends, 5)
+    del ends
+    gc.collect()
+    assert gone() is not None and chunk.q_start == gone().data_ptr()
+    rows = torch.zeros(5, 1, 128)
+    monkeypatch.setattr(S, "load", lambda: type("L", (), {"santa_attend_chunk": None, "santa_rope_append": None})())
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 1 if self is gone() else 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    shape, kv = S.santa_shape_t(1, 1, 1, 128, S.SANTA_F32), S.santa_kv_t()
+    with pytest.raises(ValueError, match="one device"):
+        S.santa_attend_chunk(rows, kv, shape, chunk, None, 0.1, rows, rows)
+    with pytest.raises(ValueError, match="one device"):
+        S.santa_rope_append(rows, rows, rows, kv, shape, chunk, None, rows)
+    del chunk
+    gc.collect()
+    assert gone() is None
