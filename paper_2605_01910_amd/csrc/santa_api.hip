@@ -309,9 +309,12 @@ santa::AttendPlan make_attend_plan(const santa_shape_t *sh, const santa_kv_t *kv
   p.dtype = sh->dtype;
   p.elem = kv->kv_dtype == SANTA_KV_FP8_E4M3 ? 2 : sh->dtype == SANTA_BF16 ? 0 : 1;
   const int64_t longest = ch.max_tokens ? std::min(ch.max_tokens, ch.num_tokens) : ch.num_tokens;
-  // Few rows, up to one matrix tile's columns (us, this kernel / full tiles: one
-  // sequence over 2k keys, 32 rows 15.6 / 18.3, 48 rows in two tiles 26.7 / 18.6; 8
-  // over 4k 33.7 / 36.5, 53.6 / 37.5; 32 over 8k 176 / 212, 304 / 214).
+  // Few rows, up to one matrix tile's columns (us, this kernel / full tiles, groups of
+  // four.  bf16: one sequence over 8k keys, 32 rows 17.5 / 22.3, 128 rows 25.7 / 25.4;
+  // 8 over 4k, 32 rows 31.9 / 32.7, 48 rows in two tiles 44.3 / 33.7; 32 over 8k 172 /
+  // 209, 275 / 210.  FP8 and float32 tiles cost more per key and would gain up to 64
+  // rows: FP8, 32 over 8k, 113 / 175, 160 / 184, 128 rows 278 / 205; float32, 8 over 4k,
+  // 72.9 / 136, 108 / 140, 182 / 148, but one over 1k keys 20.7 / 16.6, 20.6 / 19.6).
   p.few = longest * p.G <= santa::kFewRows;
   p.rows = p.few ? santa::kFewRows : santa::kManyRows;
   p.tile_tokens = p.rows / p.G;
