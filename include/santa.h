@@ -406,9 +406,10 @@ size_t santa_attend_workspace_size(const santa_shape_t *shape, const santa_kv_t 
  * infinite or, where its weight rounds to zero, NaN.  Scores, sums and outputs are
  * kept in float32; over bfloat16 and FP8 caches a weight is rounded before it
  * multiplies its value, by up to 2^-14 of itself where max_tokens (num_tokens, if
- * unknown) times the group is at most 32, by up to 2^-8 (bfloat16) beyond.  Contiguous and paged caches, every kv_dtype; kv->k_new and kv->v_new
- * must be NULL.  santa_set_options: `splits` sets the key splits per tile, the
- * path is ignored. */
+ * unknown) times the group is at most 32, by up to 2^-8 (bfloat16) beyond.
+ * Contiguous and paged caches, every kv_dtype; kv->k_new and kv->v_new must be
+ * NULL.  santa_set_options: `splits` sets the key splits per tile, the path is
+ * ignored. */
 santa_status_t santa_attend_chunk(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,
                                   const santa_chunk_t *chunk, const santa_window_t *window,
                                   float scale, void *out, void *ws, size_t ws_bytes, void *stream);
@@ -422,9 +423,8 @@ santa_status_t santa_decode_window(const void *q, const santa_kv_t *kv, const sa
 /* Profiling hook (not part of the method).  start_event and stop_event are
  * hipEvent_t handles created by the caller with timing enabled.  The next
  * santa_decode_*, santa_rope_append or santa_attend_chunk (or santa_stream_read)
- * call made on the calling thread attaches them to its own kernels: the GPU records start_event when the
- * call's first kernel is
- * dispatched and stop_event when its last kernel completes, so
+ * call made on the calling thread attaches them to its own kernels: the GPU
+ * records start_event when the call's first kernel is dispatched and stop_event when its last kernel completes, so
  * hipEventElapsedTime(start, stop) is the call's execution time on the device
  * without host launch latency.  One-shot: that call consumes the request even
  * if it fails validation.  (NULL, NULL) cancels a pending request; exactly one

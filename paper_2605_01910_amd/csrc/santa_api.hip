@@ -276,7 +276,8 @@ constexpr int64_t kMaxWorkgroups = UINT32_MAX / santa::kThreads;
 // Whether both launches of the plan count their threads in 32 bits (a wave per row that is joined).
 bool attend_fits(const santa::AttendPlan &p) {
   const int64_t groups = p.grid_tiles * p.Hkv;
-  return groups * p.T <= kMaxWorkgroups && (p.T == 1 || p.join || groups * p.rows / (santa::kThreads / 64) <= kMaxWorkgroups);
+  return groups * p.T <= kMaxWorkgroups &&
+         (p.T == 1 || p.join || groups * p.rows / (santa::kThreads / 64) <= kMaxWorkgroups);
 }
 
 // Chunk of new tokens (NULL: one per sequence).
@@ -459,7 +460,8 @@ long double rope_turns(const santa_rope_params_t &r, int i) {
   if (r.scaling == SANTA_ROPE_LINEAR) keep = 0;
   if (r.scaling == SANTA_ROPE_BANDS) keep = (r.original_len * f / pi2 - r.low) / ((long double)r.high - r.low);
   if (r.scaling == SANTA_ROPE_RAMP) {
-    auto pair = [&](double turns) { return R * std::log(r.original_len / (pi2 * turns)) / (2 * std::log((long double)r.theta)); };
+    const long double ln = std::log((long double)r.theta);
+    auto pair = [&](double turns) { return R * std::log(r.original_len / (pi2 * turns)) / (2 * ln); };
     const long double lo = std::max(0.0L, std::floor(pair(r.high))), hi = std::min(R - 1, std::ceil(pair(r.low)));
     keep = 1 - (i - lo) / std::max(hi - lo, 0.001L);
   }

@@ -526,10 +526,11 @@ __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0
 // the tiles to expect; where a batch may have more (MORE: rows enough for chunks
 // longer than max_tokens says), each workgroup goes on with the others in turn, a
 // tile at a time and unsplit, so that only the tiles to expect need room for
-// partial results: the (split, tile) workgroups of a KV head share out the rest.  A grid for all that there may be would spend its time on empty workgroups:
-// one token with 2000 padding rows over 2k keys 13.7 us, 91.7 with a workgroup for
-// every tile that the rows could make.  (Without the loop 11.1 us for 12.0 in one
-// user's window.)
+// partial results: the (split, tile) workgroups of a KV head share out the rest.
+// A grid for all that there may be would spend its time on empty workgroups: one
+// token with 2000 padding rows over 2k keys 13.7 us, 91.7 with a workgroup for every
+// tile that the rows could make.  (Without the loop 11.1 us for 12.0 in one user's
+// window.)
 struct Work {
   TileAt at;
   int kvh, rows, p_lo;     // rows: valid ones; p_lo: position of the tile's first token
@@ -644,9 +645,9 @@ __device__ __forceinline__ void add_nonfinite(const AttendArgs &a, const Work &w
 //
 // What bounds it: a wave's 64 keys x 32 rows take the matrix cores 1024 cycles, the
 // vector unit about 900 (an exponential is 16 of them) and 48 operand reads from
-// LDS; two waves per SIMD overlap these in part.  An 8k prompt runs at 0.98 to 1.0
-// PFLOP/s, 542 to 565 us, at the 2.0 GHz that this load holds (left out, the operand reads give 30 %
-// of the time, the softmax 20, the copies 17).
+// LDS; two waves per SIMD overlap these in part.  An 8k prompt runs at 0.92 to 0.98
+// PFLOP/s, 558 to 597 us from card to card, at the 2.0 GHz that this load holds (left
+// out, the operand reads give 30 % of the time, the softmax 20, the copies 17).
 //
 // Measured at a time of 600 us and not taken: 64 rows per wave at one wave per SIMD, the
 // values of a tile added while the next one's scores become weights (1049 us: the
