@@ -407,8 +407,8 @@ size_t santa_attend_workspace_size(const santa_shape_t *shape, const santa_kv_t 
  * kept in float32; over bfloat16 and FP8 caches a weight is rounded before it
  * multiplies its value, by up to 2^-14 of itself where max_tokens (num_tokens, if
  * unknown) times the group is at most 32, by up to 2^-8 (bfloat16) beyond.
- * Contiguous and paged caches, every kv_dtype; kv->k_new and kv->v_new must be
- * NULL.  santa_set_options: `splits` sets the key splits per tile, the path is
+ * Contiguous and paged caches of up to 2^30 keys, every kv_dtype; kv->k_new and
+ * kv->v_new must be NULL.  santa_set_options: `splits` sets the key splits per tile, the path is
  * ignored. */
 santa_status_t santa_attend_chunk(const void *q, const santa_kv_t *kv, const santa_shape_t *shape,
                                   const santa_chunk_t *chunk, const santa_window_t *window,

@@ -271,6 +271,12 @@ santa_status_t check_ws(const santa::Plan &p, void *ws, size_t ws_bytes) { retur
 
 bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15; }
 
+// The attention numbers keys in 32 bits and steps past the last of a split by a tile.
+santa_status_t check_attend_keys(const santa_kv_t *kv) {
+  if (kv->n_k > (1 << 30)) return fail(SANTA_ERR_UNSUPPORTED, "n_k must be at most 2^30");
+  return SANTA_OK;
+}
+
 constexpr int64_t kMaxWorkgroups = UINT32_MAX / santa::kThreads;
 
 // Whether both launches of the plan count their threads in 32 bits (a wave per row that is joined).
@@ -415,6 +421,7 @@ santa_status_t attend(const void *q, const santa_kv_t *kv, const santa_shape_t *
   santa_chunk_t ch;
   santa_status_t s = check_shape(sh);
   if (s == SANTA_OK) s = check_kv(kv, sh, true, false);
+  if (s == SANTA_OK) s = check_attend_keys(kv);
   if (s == SANTA_OK) s = check_chunk(chunk, sh, &ch);
   if (s == SANTA_OK) s = check_window(win);
   if (s != SANTA_OK) return s;
@@ -782,7 +789,8 @@ size_t santa_attend_workspace_size(const santa_shape_t *shape, const santa_kv_t 
                                    const santa_window_t *window) {
   santa_chunk_t ch;
   if (check_shape(shape) != SANTA_OK || !kv || check_kv_kind(kv, shape) != SANTA_OK ||
-      check_chunk(chunk, shape, &ch) != SANTA_OK || check_window(window) != SANTA_OK)
+      check_attend_keys(kv) != SANTA_OK || check_chunk(chunk, shape, &ch) != SANTA_OK ||
+      check_window(window) != SANTA_OK)
     return 0;
   const santa::AttendPlan p = make_attend_plan(shape, kv, ch, window);
   return attend_fits(p) ? p.total : 0;

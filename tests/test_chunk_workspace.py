@@ -67,3 +67,14 @@ def test_no_size_for_calls_that_are_refused():
         sh = S.santa_shape_t(2, 8, 2, 128, dtype)
         assert (S.load().santa_attend_workspace_size(ref(sh), ref(kv), None, None) > 0) == fine
     assert size(Hq=2 ** 24 + 8, Hkv=2 ** 24 + 8, n_k=1) == 0
+
+
+def test_more_keys_than_32_bits_number_are_refused():
+    """A contiguous cache whose rows share memory (stride 0) or a table that names one page throughout
+    can have as many keys as n_k says."""
+    sh, ch = S.santa_shape_t(2, 8, 2, 128, 0), S.santa_chunk_t(16, 10, 5)
+    for n_k, fine in ((2 ** 30, True), (2 ** 30 + 1, False), (2 ** 31 - 1, False)):
+        kv = S.santa_kv_t(16, 16, 0, 0, 128, None, None, 0, 0, n_k)
+        status = S.SANTA_ERR_WORKSPACE if fine else S.SANTA_ERR_UNSUPPORTED
+        assert S.load().santa_attend_chunk(16, ref(kv), ref(sh), ref(ch), None, 0.1, 16, None, 0, None) == status
+        assert (S.load().santa_attend_workspace_size(ref(sh), ref(kv), ref(ch), None) > 0) == fine
